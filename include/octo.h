@@ -450,6 +450,136 @@ OCTO_API int octo_postprocess_frame_static(int32_t device, const float* d_head, 
  * Allocates nothing.  (Part of the same addition; no counterpart in the paper.) */
 OCTO_API int octo_static_status(int32_t device, uint32_t* status_word, void* cuda_stream);
 
+/* ---- tokens of a transformer behind the stage -----------------------------------------------
+ * A downstream model may be a transformer that takes every crop (or the detector's canvas) as patches and
+ * lets the tokens of one set attend to the states of another: a crop's tokens to the frame the crop was cut
+ * from, one new token to the states of its crop, questions to the states of a clip.  How many items a frame
+ * has and where they lie is known on the device only (Section III-B, Observation 1: what a detector emits
+ * is what its downstream models receive), so the calls below take the stage's item table, offsets and
+ * counts as they lie there: nothing synchronises, and every call may be captured into a CUDA graph.
+ * They hold no state: any number of them may run at once on different streams, each with its own workspace.
+ * `device` is the ordinal that all of a call's pointers belong to; the calling thread's current device is
+ * left as it was.  Strides count elements, offsets are computed in 64 bits. */
+
+/* Element types of the token calls. */
+#define OCTO_F16 0
+#define OCTO_BF16 1
+#define OCTO_F32 2
+
+/*
+ * Where the patches of packed crops lie in time and in their source frames.
+ *   d_items    device, [max_items] records of an item table (octo_stage_item_table, or records that the
+ *              caller wrote: the letterboxed canvas of a frame is an item whose rectangle is the whole
+ *              frame, with keep_aspect = 1).  4-byte aligned.
+ *   d_n_items  device, or NULL: only the first min(max_items, *d_n_items) records count (the {packed, total}
+ *              of octo_crop_batch); what belongs to the others is left as it was.
+ *   slot_w, slot_h, patch  size of the crop and side of a patch in pixels (1 .. 2048); patch divides both.
+ *   keep_aspect  how the rectangle was fitted into the slot (octo_branch_cfg_t).
+ *   d_times    device, [n_frames] float32 time of every frame, or NULL: time 0.
+ *   d_positions  device, [max_items, (slot_h / patch) * (slot_w / patch), 3] float32: (time, y, x) of the
+ *              patch's centre in source-frame pixels, x = rx0 + ((2 i + 1) patch - 2 pad_l) * cw / (2 nw)
+ *              for the image of nw columns that starts at column pad_l of the slot (plain stretch: the
+ *              whole slot), evaluated in 64 bits and rounded once; y likewise.
+ *   d_visible  device, [max_items, patches] uint8 or NULL: 1 where the patch shows a pixel of the image,
+ *              0 where it shows canvas only.
+ * A record that has an empty rectangle, or names a frame outside [0, n_frames), gets zeros in both.
+ * Errors: OCTO_E_INVALID_ARG, OCTO_E_ALIGNMENT (pointers not multiples of 4 bytes), OCTO_E_CUDA.
+ */
+OCTO_API int octo_patch_positions(int32_t device, const octo_item_t* d_items, int32_t max_items, const int32_t* d_n_items,
+                                  int32_t slot_w, int32_t slot_h, int32_t patch, int32_t keep_aspect,
+                                  const float* d_times, int32_t n_frames, float* d_positions, uint8_t* d_visible,
+                                  void* cuda_stream);
+
+/* The same for the crops that the last octo_crop_batch of `branch` packed: its item table, its packed count,
+ * its slot size and fit.  max_items as in that call (or fewer).  d_times: one time per frame of the batch, or
+ * NULL.  Errors: as above, plus OCTO_E_NO_POSTPROCESS (the branch has not been cropped yet). */
+OCTO_API int octo_stage_patch_positions(octo_stage_t* st, int32_t branch, int32_t max_items, int32_t patch,
+                                        const float* d_times, float* d_positions, uint8_t* d_visible,
+                                        void* cuda_stream);
+
+/* One tensor [rows, heads, head_dim] of a token call; the elements of a head lie side by side. */
+typedef struct {
+    void* d_data;
+    int64_t row_stride, head_stride; /* elements */
+} octo_heads_t;
+
+/*
+ * Norm of every query and key head and its rotation by the token's position, in one pass.
+ * For a head x of head_dim elements: y = x * rsqrt(mean(x^2) + eps) * weight (no weight: y = x); then pair i
+ * of the first 2 * pairs elements, (i, i + pairs) or with `interleaved` (2 i, 2 i + 1), is turned by the angle
+ * position[axis[i]] * freq[i]: (y0 cos - y1 sin, y1 cos + y0 sin); elements from 2 * pairs on stay y.
+ * The angle is reduced in 64 bits (a position of 2^24 and a frequency of 1 still have a phase that is good to
+ * binary32); everything else is binary32, rounded once to the type of the tensors.
+ */
+typedef struct {
+    int32_t device, dtype;            /* OCTO_F16, OCTO_BF16 or OCTO_F32                                   */
+    int32_t heads, kv_heads;          /* heads of q and of k, 0 .. 16384 each; at least one in all         */
+    int32_t head_dim, pairs;          /* head_dim: even, 2 .. 256; 0 <= 2 * pairs <= head_dim              */
+    int32_t interleaved;              /* 1: pairs are neighbours; 0: the halves of the first 2 * pairs     */
+    int32_t num_axes;                 /* positions per token, 1 .. 8                                       */
+    int32_t positions_are_int;        /* 1: d_positions holds int32, 0: float32                            */
+    int32_t _pad;
+    int64_t rows;                     /* tokens                                                            */
+    octo_heads_t q, k, q_out, k_out;  /* an output may be its input; else they do not overlap              */
+    const void* d_q_weight;           /* [head_dim] of the tensors' type, or NULL: no norm                 */
+    const void* d_k_weight;
+    const void* d_positions;          /* [rows, num_axes]                                                  */
+    const float* d_freqs;             /* [pairs]                                                           */
+    const int32_t* d_axes;            /* [pairs], axis of every pair; a value outside turns nothing        */
+    const int32_t* d_n_items;         /* or NULL: rows from *d_n_items * item_rows on are left as they were */
+    int64_t item_rows;
+    float eps;                        /* >= 0                                                              */
+    float _pad2;
+} octo_rotate_t;
+
+/* Errors: OCTO_E_INVALID_ARG, OCTO_E_ALIGNMENT (a pointer not a multiple of its element's size), OCTO_E_CUDA. */
+OCTO_API int octo_norm_rotate(const octo_rotate_t* args, void* cuda_stream);
+
+/*
+ * Attention of one set of tokens to another set's states, segment by segment.
+ * Segment s has the query rows [q0, q1) and the key rows [k0, k1), where q0 = (b - q_first) * q_rows with
+ * b = d_q_offsets[s], q1 the same of d_q_offsets[s + 1], both clipped to [0, q_total]; without d_q_offsets b is
+ * s itself, so that every segment has q_rows rows.  Keys likewise.  With the d_offsets of octo_crop_batch and
+ * q_rows tokens per crop, segment f is the crops of frame f.  Query segments do not overlap, and `out` shares no
+ * memory with the inputs.
+ *   out[r, h] = sum_j softmax_j(scale * q[r, h] . k[j, h']) v[j, h'],  h' = h / (heads / kv_heads),
+ * over the key rows j of r's segment with d_key_mask[j] != 0 (no mask: all of them); 0 where there is none.
+ * Hidden keys and values are never looked at: they may hold NaN or infinities.  Rows of no segment are left
+ * as they were.  Scores, the softmax and the sums are binary32; the weights are rounded to the tensors' type
+ * before they meet the values, as the tensor cores take them; one rounding at the end.
+ */
+typedef struct {
+    int32_t device, dtype;            /* OCTO_F16 or OCTO_BF16                                             */
+    int32_t segments;                 /* >= 1 (with d_q_offsets at most OCTO_MAX_SEGMENTS)                 */
+    int32_t heads, kv_heads;          /* kv_heads divides heads                                            */
+    int32_t head_dim;                 /* a multiple of 8, 8 .. 128                                         */
+    int64_t q_total, k_total;         /* rows of q and out; rows of k, v and the mask: at most 2^30, and   */
+                                      /* q_total * heads < 2^31                                            */
+    octo_heads_t q, k, v, out;        /* 16-byte aligned, strides multiples of 8 elements                  */
+    const int32_t* d_q_offsets;       /* [segments + 1] non-decreasing, or NULL                            */
+    const int32_t* d_k_offsets;       /* [segments + 1] non-decreasing, or NULL                            */
+    int64_t q_rows, k_rows;           /* rows per step of the offsets, >= 1                                */
+    int64_t q_first, k_first;
+    int64_t max_q, max_k;             /* most query / key rows of a segment; rows of a longer segment from */
+                                      /* there on are left / not looked at.  0: not known                  */
+    const uint8_t* d_key_mask;        /* [k_total] or NULL                                                 */
+    float scale;                      /* finite                                                            */
+    float _pad;
+    uint32_t* d_status;               /* one word, or NULL: OCTO_STATUS_COPY_TIMEOUT is set (and the rows  */
+                                      /* concerned become NaN) if a bounded wait of the kernel gives up    */
+} octo_attend_t;
+
+#define OCTO_MAX_SEGMENTS 4096
+
+/* Bytes of workspace that octo_cross_attention needs for these arguments (pointers are not looked at); 0 where
+ * no work is split over the keys. */
+OCTO_API int octo_attend_workspace(const octo_attend_t* args, int64_t* bytes);
+
+/* d_workspace: device, at least that many bytes, 16-byte aligned; its contents mean nothing between calls.
+ * Errors: OCTO_E_INVALID_ARG, OCTO_E_CAPACITY (too many segments, a workspace that is too small),
+ * OCTO_E_ALIGNMENT, OCTO_E_CUDA. */
+OCTO_API int octo_cross_attention(const octo_attend_t* args, void* d_workspace, int64_t workspace_bytes, void* cuda_stream);
+
 /* ---- placement of model instances on GPU inference streams (host only) ---------------------
  * The paper's co-location scheduler (Section III-C "Inference Stream", Algorithm 2): a GPU runs
  * several streams side by side; an execution occupies a portion of one stream, as long as its

@@ -42,6 +42,10 @@ OCTO_STATUS_BOUNDS = 0x20
 
 OCTO_HEAD_ROWS = 0
 OCTO_HEAD_PLANES = 1
+OCTO_F16 = 0
+OCTO_BF16 = 1
+OCTO_F32 = 2
+OCTO_MAX_SEGMENTS = 4096
 HEAD_LAYOUTS = {"rows": OCTO_HEAD_ROWS, "planes": OCTO_HEAD_PLANES}
 
 EXPORTS = (
@@ -54,6 +58,8 @@ EXPORTS = (
     "octo_queue_pop_due", "octo_coral_schedule", "octo_queue_set_options",
     "octo_adopt_items_device", "octo_stage_selftest_wait", "octo_static_status",
     "octo_stage_set_nms_cluster", "octo_stage_last_nms_cluster", "octo_stage_last_nms_half_ctas",
+    "octo_patch_positions", "octo_stage_patch_positions", "octo_norm_rotate", "octo_attend_workspace",
+    "octo_cross_attention",
 )
 
 
@@ -105,6 +111,33 @@ class CoralGpu(ctypes.Structure):
 class CoralPlacement(ctypes.Structure):
     _fields_ = [("gpu", ctypes.c_int32), ("stream", ctypes.c_int32), ("start_us", ctypes.c_int64),
                 ("end_us", ctypes.c_int64), ("duty_cycle_us", ctypes.c_int64)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("d_data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class Rotate(ctypes.Structure):
+    _fields_ = [("device", ctypes.c_int32), ("dtype", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("pairs", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("positions_are_int", ctypes.c_int32),
+                ("_pad", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("q", Heads), ("k", Heads), ("q_out", Heads), ("k_out", Heads),
+                ("d_q_weight", ctypes.c_void_p), ("d_k_weight", ctypes.c_void_p), ("d_positions", ctypes.c_void_p),
+                ("d_freqs", ctypes.c_void_p), ("d_axes", ctypes.c_void_p), ("d_n_items", ctypes.c_void_p),
+                ("item_rows", ctypes.c_int64), ("eps", ctypes.c_float), ("_pad2", ctypes.c_float)]
+
+
+class Attend(ctypes.Structure):
+    _fields_ = [("device", ctypes.c_int32), ("dtype", ctypes.c_int32), ("segments", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("q_total", ctypes.c_int64), ("k_total", ctypes.c_int64),
+                ("q", Heads), ("k", Heads), ("v", Heads), ("out", Heads),
+                ("d_q_offsets", ctypes.c_void_p), ("d_k_offsets", ctypes.c_void_p),
+                ("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64), ("q_first", ctypes.c_int64),
+                ("k_first", ctypes.c_int64), ("max_q", ctypes.c_int64), ("max_k", ctypes.c_int64),
+                ("d_key_mask", ctypes.c_void_p), ("scale", ctypes.c_float), ("_pad", ctypes.c_float),
+                ("d_status", ctypes.c_void_p)]
 
 
 REGION_DTYPE = np.dtype([("d_data", "<u8"), ("width", "<i4"), ("height", "<i4"), ("pitch_bytes", "<i4"),
@@ -193,6 +226,14 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.octo_queue_pop_due.argtypes = [vp, i32, i32, vp, vp, vp, vp]
     lib.octo_queue_pop_due.restype = ctypes.c_int
     for name in ("octo_queue_create", "octo_queue_destroy", "octo_queue_push", "octo_queue_pop"):
+        getattr(lib, name).restype = ctypes.c_int
+    lib.octo_patch_positions.argtypes = [i32, vp, i32, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp]
+    lib.octo_stage_patch_positions.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp]
+    lib.octo_norm_rotate.argtypes = [ctypes.POINTER(Rotate), vp]
+    lib.octo_attend_workspace.argtypes = [ctypes.POINTER(Attend), ctypes.POINTER(ctypes.c_int64)]
+    lib.octo_cross_attention.argtypes = [ctypes.POINTER(Attend), vp, ctypes.c_int64, vp]
+    for name in ("octo_patch_positions", "octo_stage_patch_positions", "octo_norm_rotate", "octo_attend_workspace",
+                 "octo_cross_attention"):
         getattr(lib, name).restype = ctypes.c_int
     lib.octo_coral_schedule.argtypes = [ctypes.POINTER(CoralInstance), i32, ctypes.POINTER(CoralGpu), i32,
                                         ctypes.POINTER(CoralPlacement)]
@@ -347,6 +388,7 @@ class Stage:
         self.device = torch.device("cuda", self.cfg.device)
         self.n = 0
         self._frames_keepalive: List = []
+        self._n_items_keepalive: dict = {}
         self._lib = load_library()
         self._current_stream = _stream_getter(torch, self.device)
         self._frame_array = (Frame * self.cfg.max_batch)()  # refilled by every preprocess call
@@ -471,7 +513,35 @@ class Stage:
                                        n_items.data_ptr(), self._stream(stream))
         if rc != OCTO_OK:
             raise OctoError(rc, "octo_crop_batch")
+        self._n_items_keepalive[branch] = n_items  # patch_positions and a chained stage read it on the device
         return out, offsets, n_items
+
+    def patch_positions(self, branch, max_items, patch, times=None, positions=None, visible=None, stream=None):
+        """Where the patches of the crops that the last crop call of `branch` packed lie in time and in their
+        source frames.  times: float32 CUDA tensor, one per frame of the batch, or None.  Returns (positions
+        float32 [max_items, patches, 3] as (time, y, x), visible uint8 [max_items, patches]); rows of slots that
+        no item fills are not written."""
+        t = self._torch
+        br = self.cfg.branch[branch]
+        if patch < 1 or br.out_w % patch or br.out_h % patch:
+            raise OctoError(OCTO_E_INVALID_ARG, "octo_stage_patch_positions (the patch does not divide the crop)")
+        patches = (br.out_w // patch) * (br.out_h // patch)
+        if times is not None and (times.dtype != t.float32 or times.numel() < self.n or not times.is_contiguous()
+                                  or times.device != self.device):
+            raise OctoError(OCTO_E_INVALID_ARG, "octo_stage_patch_positions (times is not a float32 vector, one per frame)")
+        if positions is None:
+            positions = t.empty((max_items, patches, 3), dtype=t.float32, device=self.device)
+        if visible is None:
+            visible = t.empty((max_items, patches), dtype=t.uint8, device=self.device)
+        for b, dtype, count in ((positions, t.float32, 3 * max_items * patches), (visible, t.uint8, max_items * patches)):
+            if b.dtype != dtype or b.numel() < count or not b.is_contiguous() or b.device != self.device:
+                raise OctoError(OCTO_E_INVALID_ARG, "octo_stage_patch_positions (an output has another shape)")
+        rc = self._lib.octo_stage_patch_positions(self.handle, branch, max_items, patch,
+                                                  None if times is None else times.data_ptr(), positions.data_ptr(),
+                                                  visible.data_ptr(), self._stream(stream))
+        if rc != OCTO_OK:
+            raise OctoError(rc, "octo_stage_patch_positions")
+        return positions, visible
 
     def item_table(self, branch: int, count: int) -> np.ndarray:
         """Host copy of the first `count` entries of the branch's item table (synchronises)."""

@@ -1,0 +1,478 @@
+// Attention of one set of tokens to another set's states (include/octo.h): the plan of a call, the kernel for
+// few query rows, and the kernel that joins work split over the keys.
+#include <math.h>
+
+#include "octo_attend.cuh"
+
+namespace octo {
+
+// ---------------------------------------------------------------------------------------
+// Few query rows (one new token per item): bound by reading every key and value once.  A CTA takes 16 rows --
+// pairs (query row, head) that share a key head -- of one segment and one split; each of its warps walks over
+// the keys in groups of 16, four warps side by side, with a softmax of its own that the warps join at the end.
+// Keys and values go from global memory straight into the operand registers of the matrix instruction: which
+// element of a head an operand's slot holds is free as long as both operands agree, so the slots are dealt out
+// such that a lane's part of a key is 16 bytes in a row, and a lane's part of the values the same 16 bytes of
+// four keys, paired up by byte permutes.  No shared memory, no barrier before the end; the loads of the next
+// group are in flight while the current one is worked on.
+// ---------------------------------------------------------------------------------------
+constexpr int kStepThreads = 128;
+constexpr int kStepWarps = kStepThreads / 32;
+constexpr int kStepRows = 16;
+constexpr int kStepKeys = 16 * kStepWarps;  // keys a CTA takes per turn
+
+template <typename T>
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                          uint32_t b1);
+template <>
+__device__ __forceinline__ void mma_16816<__half>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                                  uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma_16816<__nv_bfloat16>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                                         uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint4 ldg128(const void* p, bool take) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);  // a hidden key counts as zeros, whatever its place holds
+    if (take) asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+// DB: 64-element blocks of a head.
+template <typename T, int DB>
+__global__ void __launch_bounds__(kStepThreads)
+attend_step_kernel(const __grid_constant__ AttendArgs a, int row_tiles) {
+    constexpr int KB = 2 * DB;  // 32-element blocks
+    constexpr int SP = DB * 64 + 4;
+    __shared__ float s_o[kStepWarps][kStepRows][SP];
+    __shared__ float s_m[kStepWarps][kStepRows], s_l[kStepWarps][kStepRows];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    unsigned x = blockIdx.x;
+    const int split = (int)(x % (unsigned)a.splits);
+    x /= (unsigned)a.splits;
+    const int tile = (int)(x % (unsigned)row_tiles);
+    x /= (unsigned)row_tiles;
+    const int kvh = (int)(x % (unsigned)a.kv_heads), seg_no = (int)(x / (unsigned)a.kv_heads);
+    pdl_wait();
+    const Segment seg = segment_of(a, seg_no);
+    const int rows = seg.qn * a.group;
+    if (tile * kStepRows >= rows) return;
+    const int kb = min(split * a.chunk, seg.kn), ke = min(kb + a.chunk, seg.kn);
+    if (split > 0 && kb >= ke) return;
+    const int active = a.splits == 1 ? 1 : (seg.kn + a.chunk - 1) / a.chunk;
+
+    // queries: rows g and g + 8 of the tile, 8 elements at 32 b + 8 t of each
+    uint4 qa[KB], qb[KB];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int vr = tile * kStepRows + g + 8 * half;
+        const int row = vr / a.group, head = kvh * a.group + (vr - row * a.group);
+        const T* p = static_cast<const T*>(a.q) + (seg.q0 + row) * a.q_row + head * a.q_head;
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+            const int d = 32 * b + 8 * t;
+            (half ? qb : qa)[b] = ldg128(p + d, vr < rows && d < a.dim);
+        }
+    }
+
+    const T* const kp = static_cast<const T*>(a.k) + kvh * a.k_head + 8 * t;
+    const T* const vp = static_cast<const T*>(a.v) + kvh * a.v_head + 8 * g;
+    const uint8_t* const mp = a.mask ? a.mask + seg.k0 : nullptr;
+    auto bits_of = [&](int key) -> unsigned {  // one bit per key of the group that counts
+        const int at = key + lane;
+        bool seen = lane < 16 && at < ke;
+        if (seen && mp) seen = mp[at] != 0;
+        return __ballot_sync(0xffffffffu, seen);
+    };
+    uint4 kr[2][KB], vr[4][DB];
+    auto load_k = [&](int key, unsigned bits) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const T* p = kp + (seg.k0 + key + 8 * j + g) * a.k_row;
+            const bool seen = (bits >> (8 * j + g)) & 1u;
+#pragma unroll
+            for (int b = 0; b < KB; ++b) kr[j][b] = ldg128(p + 32 * b, seen && 32 * b + 8 * t < a.dim);
+        }
+    };
+    auto load_v = [&](int key, unsigned bits) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int n = 2 * t + (j & 1) + 8 * (j >> 1);
+            const T* p = vp + (seg.k0 + key + n) * a.v_row;
+            const bool seen = (bits >> n) & 1u;
+#pragma unroll
+            for (int b = 0; b < DB; ++b) vr[j][b] = ldg128(p + 64 * b, seen && 64 * b + 8 * g < a.dim);
+        }
+    };
+
+    float o[DB * 8][4];
+#pragma unroll
+    for (int i = 0; i < DB * 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;  // rows g and g + 8
+
+    int key = kb + 16 * warp;
+    unsigned bits = bits_of(key);
+    load_k(key, bits);
+    load_v(key, bits);
+    unsigned next = bits_of(key + kStepKeys);
+    for (; key < ke; key += kStepKeys) {
+        const unsigned after = bits_of(key + 2 * kStepKeys);
+        if (bits == 0) {  // nothing to see: only fetch the next group
+            load_k(key + kStepKeys, next);
+            load_v(key + kStepKeys, next);
+            bits = next;
+            next = after;
+            continue;
+        }
+        float s[2][4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.0f;
+#pragma unroll
+            for (int b = 0; b < KB; ++b) {
+                mma_16816<T>(s[j], qa[b].x, qb[b].x, qa[b].y, qb[b].y, kr[j][b].x, kr[j][b].y);
+                mma_16816<T>(s[j], qa[b].z, qb[b].z, qa[b].w, qb[b].w, kr[j][b].z, kr[j][b].w);
+            }
+        }
+        load_k(key + kStepKeys, next);
+        // scores of this lane: keys 8 j + 2 t and + 1, rows g (0, 1) and g + 8 (2, 3)
+        float t0 = -INFINITY, t1 = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[j][i] = (bits >> (8 * j + 2 * t + (i & 1))) & 1u ? s[j][i] * a.scale_log2 : -INFINITY;
+                if (i < 2) t0 = fmaxf(t0, s[j][i]);
+                else t1 = fmaxf(t1, s[j][i]);
+            }
+        t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, 1));
+        t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, 1));
+        t0 = fmaxf(m0, fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, 2)));
+        t1 = fmaxf(m1, fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, 2)));
+        const float r0 = t0 == -INFINITY ? 0.0f : t0, r1 = t1 == -INFINITY ? 0.0f : t1;
+        if (__any_sync(0xffffffffu, t0 != m0 || t1 != m1)) {  // a larger maximum: what was summed shrinks
+            const float f0 = ex2(m0 - r0), f1 = ex2(m1 - r1);
+            l0 *= f0;
+            l1 *= f1;
+#pragma unroll
+            for (int i = 0; i < DB * 8; ++i) {
+                o[i][0] *= f0;
+                o[i][1] *= f0;
+                o[i][2] *= f1;
+                o[i][3] *= f1;
+            }
+            m0 = t0;
+            m1 = t1;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            s[j][0] = ex2(s[j][0] - r0);
+            s[j][1] = ex2(s[j][1] - r0);
+            s[j][2] = ex2(s[j][2] - r1);
+            s[j][3] = ex2(s[j][3] - r1);
+            l0 += s[j][0] + s[j][1];
+            l1 += s[j][2] + s[j][3];
+        }
+        // the weights in the type of the values: what the matrix instruction takes (the sum keeps them unrounded)
+        const uint32_t p0 = pack2<T>(s[0][0], s[0][1]), p1 = pack2<T>(s[0][2], s[0][3]);
+        const uint32_t p2 = pack2<T>(s[1][0], s[1][1]), p3 = pack2<T>(s[1][2], s[1][3]);
+#pragma unroll
+        for (int b = 0; b < DB; ++b) {
+            const uint32_t* v0 = reinterpret_cast<const uint32_t*>(&vr[0][b]);
+            const uint32_t* v1 = reinterpret_cast<const uint32_t*>(&vr[1][b]);
+            const uint32_t* v2 = reinterpret_cast<const uint32_t*>(&vr[2][b]);
+            const uint32_t* v3 = reinterpret_cast<const uint32_t*>(&vr[3][b]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const unsigned pick = i & 1 ? 0x7632u : 0x5410u;
+                mma_16816<T>(o[8 * b + i], p0, p1, p2, p3, __byte_perm(v0[i / 2], v1[i / 2], pick),
+                             __byte_perm(v2[i / 2], v3[i / 2], pick));
+            }
+        }
+        load_v(key + kStepKeys, next);
+        bits = next;
+        next = after;
+    }
+
+    // join the warps: o[8 b + i] of this lane are elements 64 b + 16 t + i (0, 2) and + 8 (1, 3) of rows g and g + 8
+    l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
+    l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
+    l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
+    l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
+    if (t == 0) {
+        s_m[warp][g] = m0;
+        s_l[warp][g] = l0;
+        s_m[warp][g + 8] = m1;
+        s_l[warp][g + 8] = l1;
+    }
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int i = 0; i < 8; i += 4)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float4 f = make_float4(o[8 * b + i][c], o[8 * b + i + 1][c], o[8 * b + i + 2][c], o[8 * b + i + 3][c]);
+                *reinterpret_cast<float4*>(&s_o[warp][g + 8 * (c >> 1)][64 * b + 16 * t + 8 * (c & 1) + i]) = f;
+            }
+    __syncthreads();
+    const int r = threadIdx.x >> 3, vrow = tile * kStepRows + r;
+    if (vrow >= rows) return;
+    float top = s_m[0][r];
+#pragma unroll
+    for (int w = 1; w < kStepWarps; ++w) top = fmaxf(top, s_m[w][r]);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float share[kStepWarps], sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kStepWarps; ++w) {
+        share[w] = ex2(s_m[w][r] - ref);
+        sum += share[w] * s_l[w][r];
+    }
+    const int row = vrow / a.group, head = kvh * a.group + (vrow - row * a.group);
+    const int64_t part = ((int64_t)split * a.q_total + seg.q0 + row) * a.heads + head;
+    const bool last = active <= 1;
+    const float inv = last ? (sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f) : 1.0f;
+    T* out = static_cast<T*>(a.out) + (seg.q0 + row) * a.o_row + head * a.o_head;
+#pragma unroll
+    for (int b = 0; b < DB; ++b) {
+        const int d = 64 * b + 8 * (threadIdx.x & 7);
+        if (d >= a.dim) continue;
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            f[i] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kStepWarps; ++w) f[i] += share[w] * s_o[w][r][d + i];
+            f[i] *= inv;
+        }
+        if (last) {
+            uint4 y;
+            y.x = pack2<T>(f[0], f[1]);
+            y.y = pack2<T>(f[2], f[3]);
+            y.z = pack2<T>(f[4], f[5]);
+            y.w = pack2<T>(f[6], f[7]);
+            *reinterpret_cast<uint4*>(out + d) = y;
+        } else {
+            float4* p = reinterpret_cast<float4*>(a.part_o + part * a.dim + d);
+            p[0] = make_float4(f[0], f[1], f[2], f[3]);
+            p[1] = make_float4(f[4], f[5], f[6], f[7]);
+        }
+    }
+    if (!last && (threadIdx.x & 7) == 0) a.part_ml[part] = make_float2(top, sum);
+}
+
+// ---------------------------------------------------------------------------------------
+// Joins the splits of a row: a warp per (query row, head), four elements of it per lane, the splits in order.
+// ---------------------------------------------------------------------------------------
+constexpr int kJoinThreads = 256;
+
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads)
+attend_join_kernel(const __grid_constant__ AttendArgs a) {
+    pdl_wait();
+    const int64_t at = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) >> 5;  // row * heads + head
+    const int lane = threadIdx.x & 31;
+    if (at >= a.q_total * a.heads) return;
+    const int64_t row = at / a.heads;
+    const int head = (int)(at - row * a.heads);
+    // the segment this row belongs to
+    const int64_t step = row / a.q_rows + a.q_first;
+    int s;
+    if (a.q_offsets) {
+        int lo = 0, hi = a.segments;  // last s with offsets[s] <= step
+        if (a.q_offsets[0] > step) return;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (a.q_offsets[mid] <= step) lo = mid; else hi = mid;
+        }
+        s = lo;
+    } else {
+        if (step < 0 || step >= a.segments) return;
+        s = (int)step;
+    }
+    const Segment seg = segment_of(a, s);
+    if (row < seg.q0 || row >= seg.q0 + seg.qn) return;
+    const int active = (seg.kn + a.chunk - 1) / a.chunk;
+    if (active <= 1) return;
+    const int64_t step_part = a.q_total * a.heads;
+    float top = -INFINITY;
+    for (int i = lane; i < active; i += 32) top = fmaxf(top, a.part_ml[i * step_part + at].x);
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+    const float ref = top == -INFINITY ? 0.0f : top;
+    const int d = 4 * lane;
+    float sum = 0.0f;
+    float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int i = 0; i < active; ++i) {
+        const float2 ml = a.part_ml[i * step_part + at];
+        const float w = ex2(ml.x - ref);
+        sum += w * ml.y;
+        if (d < a.dim) {
+            const float4 p = *reinterpret_cast<const float4*>(a.part_o + (i * step_part + at) * a.dim + d);
+            f.x += w * p.x;
+            f.y += w * p.y;
+            f.z += w * p.z;
+            f.w += w * p.w;
+        }
+    }
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    if (d < a.dim) {
+        T* out = static_cast<T*>(a.out) + row * a.o_row + head * a.o_head + d;
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(f.x * inv, f.y * inv), pack2<T>(f.z * inv, f.w * inv));
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// The plan of a call: which kernel, and into how many splits.  It follows from sizes alone.
+// ---------------------------------------------------------------------------------------
+struct AttendPlan {
+    int64_t row_tiles;  // per segment and key head
+    int splits, chunk;
+    int64_t ctas;
+    int64_t workspace;
+};
+
+static int validate(const octo_attend_t* c) {
+    if (!c || c->device < 0) return OCTO_E_INVALID_ARG;
+    if (c->dtype != OCTO_F16 && c->dtype != OCTO_BF16) return OCTO_E_INVALID_ARG;
+    if (c->segments < 1 || c->heads < 1 || c->kv_heads < 1 || c->heads > 16384 || c->heads % c->kv_heads)
+        return OCTO_E_INVALID_ARG;
+    if (c->head_dim < 8 || c->head_dim > 128 || c->head_dim % 8) return OCTO_E_INVALID_ARG;
+    const int64_t most = 1 << 30;
+    if (c->q_total < 0 || c->k_total < 0 || c->q_total > most || c->k_total > most) return OCTO_E_INVALID_ARG;
+    if (c->q_total * c->heads > INT32_MAX) return OCTO_E_CAPACITY;
+    if (c->q_rows < 1 || c->k_rows < 1 || c->q_rows > most || c->k_rows > most) return OCTO_E_INVALID_ARG;
+    if (c->q_first < -most || c->q_first > most || c->k_first < -most || c->k_first > most) return OCTO_E_INVALID_ARG;
+    if (c->max_q < 0 || c->max_k < 0) return OCTO_E_INVALID_ARG;
+    if (!(fabsf(c->scale) <= 3e38f)) return OCTO_E_INVALID_ARG;
+    if ((c->d_q_offsets || c->d_k_offsets) && c->segments > OCTO_MAX_SEGMENTS) return OCTO_E_CAPACITY;
+    return OCTO_OK;
+}
+
+static int64_t bound_of(int64_t given, const int32_t* offsets, int64_t rows, int64_t total) {
+    int64_t b = offsets ? total : (rows < total ? rows : total);
+    if (given > 0 && given < b) b = given;
+    return b < 1 ? 1 : b;
+}
+
+static int make_plan(const octo_attend_t* c, int sms, AttendPlan* p) {
+    const int64_t group = c->heads / c->kv_heads;
+    const int64_t max_q = bound_of(c->max_q, c->d_q_offsets, c->q_rows, c->q_total);
+    const int64_t max_k = bound_of(c->max_k, c->d_k_offsets, c->k_rows, c->k_total);
+    p->row_tiles = (max_q * group + kStepRows - 1) / kStepRows;
+    if ((double)c->segments * c->kv_heads * (double)p->row_tiles > (double)INT32_MAX) return OCTO_E_CAPACITY;
+    const int64_t units = (int64_t)c->segments * c->kv_heads * p->row_tiles;
+    const int64_t rows_at_most = (c->q_total * group + kStepRows - 1) / kStepRows + c->segments;
+    const int64_t busy = units < rows_at_most * c->kv_heads ? units : rows_at_most * c->kv_heads;
+    const int64_t want = (int64_t)sms * 12;
+    int64_t splits = busy >= want ? 1 : (want + busy - 1) / busy;
+    int64_t chunk = (max_k + splits - 1) / splits;
+    if (chunk < 512) chunk = 512;
+    chunk = (chunk + kStepKeys - 1) / kStepKeys * kStepKeys;
+    splits = (max_k + chunk - 1) / chunk;
+    p->splits = (int)splits;
+    p->chunk = splits == 1 ? (int)max_k : (int)chunk;
+    p->ctas = units * splits;
+    p->workspace = splits == 1 ? 0 : splits * c->q_total * c->heads * (c->head_dim + 2) * (int64_t)sizeof(float);
+    return p->ctas > INT32_MAX || p->workspace < 0 ? OCTO_E_CAPACITY : OCTO_OK;
+}
+
+template <typename T>
+static cudaError_t launch_attend(const AttendArgs& a, const AttendPlan& p, cudaStream_t stream) {
+    auto kernel = a.dim <= 64 ? attend_step_kernel<T, 1> : attend_step_kernel<T, 2>;
+    cudaError_t e = launch_kernel(kernel, dim3((unsigned)p.ctas), dim3(kStepThreads), 0, stream, a, (int)p.row_tiles);
+    if (e == cudaSuccess && a.splits > 1) {
+        const int64_t blocks = (a.q_total * a.heads * 32 + kJoinThreads - 1) / kJoinThreads;
+        e = launch_kernel(attend_join_kernel<T>, dim3((unsigned)blocks), dim3(kJoinThreads), 0, stream, a);
+    }
+    return e;
+}
+
+}  // namespace octo
+
+using namespace octo;
+
+extern "C" int octo_attend_workspace(const octo_attend_t* c, int64_t* bytes) {
+    if (!bytes) return OCTO_E_INVALID_ARG;
+    *bytes = 0;
+    const int rc = validate(c);
+    if (rc != OCTO_OK) return rc;
+    if (c->q_total == 0) return OCTO_OK;
+    int sms = 0;
+    const cudaError_t e = sm_count_of(c->device, &sms);
+    if (e != cudaSuccess) return report_cuda_error(e, "octo_attend_workspace");
+    AttendPlan p;
+    const int prc = make_plan(c, sms, &p);
+    if (prc == OCTO_OK) *bytes = p.workspace;
+    return prc;
+}
+
+extern "C" int octo_cross_attention(const octo_attend_t* c, void* d_workspace, int64_t workspace_bytes, void* cuda_stream) {
+    const int rc = validate(c);
+    if (rc != OCTO_OK) return rc;
+    if (c->q_total == 0) return OCTO_OK;
+    if (!c->q.d_data || !c->out.d_data || (c->k_total > 0 && (!c->k.d_data || !c->v.d_data))) return OCTO_E_INVALID_ARG;
+    for (const octo_heads_t* t : {&c->q, &c->k, &c->v, &c->out})
+        if (!aligned_to(t->d_data, 16) || t->row_stride % 8 || t->head_stride % 8) return OCTO_E_ALIGNMENT;
+    if (!aligned_to(c->d_q_offsets, 4) || !aligned_to(c->d_k_offsets, 4) || !aligned_to(c->d_status, 4) ||
+        !aligned_to(d_workspace, 16))
+        return OCTO_E_ALIGNMENT;
+    DeviceScope scope(c->device);
+    if (scope.error != cudaSuccess) return report_cuda_error(scope.error, "octo_cross_attention");
+    int sms = 0;
+    cudaError_t e = sm_count_of(c->device, &sms);
+    if (e != cudaSuccess) return report_cuda_error(e, "octo_cross_attention");
+    AttendPlan p;
+    const int prc = make_plan(c, sms, &p);
+    if (prc != OCTO_OK) return prc;
+    if (p.workspace > 0 && (!d_workspace || workspace_bytes < p.workspace)) return OCTO_E_CAPACITY;
+
+    AttendArgs a;
+    a.q = c->q.d_data;
+    a.k = c->k.d_data;
+    a.v = c->v.d_data;
+    a.out = c->out.d_data;
+    a.q_row = c->q.row_stride;
+    a.q_head = c->q.head_stride;
+    a.k_row = c->k.row_stride;
+    a.k_head = c->k.head_stride;
+    a.v_row = c->v.row_stride;
+    a.v_head = c->v.head_stride;
+    a.o_row = c->out.row_stride;
+    a.o_head = c->out.head_stride;
+    a.q_offsets = c->d_q_offsets;
+    a.k_offsets = c->d_k_offsets;
+    a.q_rows = c->q_rows;
+    a.k_rows = c->k_rows;
+    a.q_first = c->q_first;
+    a.k_first = c->k_first;
+    a.q_total = c->q_total;
+    a.k_total = c->k_total;
+    a.max_q = bound_of(c->max_q, c->d_q_offsets, c->q_rows, c->q_total);
+    a.max_k = bound_of(c->max_k, c->d_k_offsets, c->k_rows, c->k_total);
+    a.mask = c->d_key_mask;
+    a.scale_log2 = (float)((double)c->scale * 1.44269504088896340736);
+    a.segments = c->segments;
+    a.heads = c->heads;
+    a.kv_heads = c->kv_heads;
+    a.group = c->heads / c->kv_heads;
+    a.dim = c->head_dim;
+    a.splits = p.splits;
+    a.chunk = p.chunk;
+    a.part_o = static_cast<float*>(d_workspace);
+    a.part_ml = p.workspace > 0 ? reinterpret_cast<float2*>(a.part_o + (int64_t)p.splits * c->q_total * c->heads * c->head_dim)
+                                : nullptr;
+    a.status = c->d_status;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    e = c->dtype == OCTO_F16 ? launch_attend<__half>(a, p, stream) : launch_attend<__nv_bfloat16>(a, p, stream);
+    return e == cudaSuccess ? OCTO_OK : report_cuda_error(e, "octo_cross_attention");
+}

@@ -246,6 +246,7 @@ extern "C" int octo_preprocess_batch(octo_stage_t* st, const octo_frame_t* frame
     }
     st->n_frames = 0;
     st->have_dets = false;
+    st->cropped_branches = 0;
     st->tab_on_device = false;
     for (int i = 0; i < n; ++i) {
         FrameDesc& fd = st->frames[i];
@@ -288,6 +289,7 @@ extern "C" int octo_adopt_regions(octo_stage_t* st, const octo_region_t* regions
     }
     st->n_frames = 0;
     st->have_dets = false;
+    st->cropped_branches = 0;
     st->tab_on_device = false;
     for (int i = 0; i < n; ++i) {
         const octo_region_t& r = regions[i];
@@ -390,6 +392,7 @@ extern "C" int octo_adopt_items_device(octo_stage_t* st, const octo_stage_t* ups
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     st->n_frames = 0;
     st->have_dets = false;
+    st->cropped_branches = 0;
     cudaError_t e;
     const int un = upstream->tab_on_device ? 1 : upstream->n_frames;
     const octo_item_t* const items = upstream->d_items[branch];
@@ -426,6 +429,7 @@ extern "C" int octo_postprocess_batch(octo_stage_t* st, const float* d_head, int
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const octo_stage_config_t& c = st->cfg;
     st->have_dets = false;
+    st->cropped_branches = 0;
     OCTO_CUDA(cudaSetDevice(c.device));
     {
         ScopedKernelTimer t(st, OCTO_K_DECODE, stream);
@@ -508,6 +512,7 @@ extern "C" int octo_postprocess_batch(octo_stage_t* st, const float* d_head, int
     }
     st->launches += 1;
     st->have_dets = true;
+    st->cropped_branches = 0;
     st->d_dets = d_dets;
     return OCTO_OK;
 }
@@ -557,7 +562,25 @@ extern "C" int octo_crop_batch(octo_stage_t* st, int32_t branch, int32_t first_i
     }
     st->launches += 1;
     st->d_last_n_items[branch] = d_n_items;
+    st->cropped_branches |= 1 << branch;
     return OCTO_OK;
+}
+
+extern "C" int octo_stage_patch_positions(octo_stage_t* st, int32_t branch, int32_t max_items, int32_t patch,
+                                          const float* d_times, float* d_positions, uint8_t* d_visible,
+                                          void* cuda_stream) {
+    if (!st || branch < 0 || branch >= st->cfg.num_branches || max_items < 0 || patch < 1) return OCTO_E_INVALID_ARG;
+    const octo_branch_cfg_t& br = st->cfg.branch[branch];
+    if (br.out_w % patch || br.out_h % patch) return OCTO_E_INVALID_ARG;
+    if (st->n_frames < 1) return OCTO_E_NO_PREPROCESS;
+    if (!((st->cropped_branches >> branch) & 1)) return OCTO_E_NO_POSTPROCESS;  // no item table of these detections yet
+    const long long cap = (long long)st->cfg.max_batch * st->cfg.max_det;
+    if (max_items > cap) max_items = (int32_t)cap;  // as octo_crop_batch: the table holds no more
+    const int rc = octo_patch_positions(st->cfg.device, st->d_items[branch], max_items, st->d_last_n_items[branch],
+                                        br.out_w, br.out_h, patch, br.keep_aspect, d_times, st->n_frames, d_positions,
+                                        d_visible, cuda_stream);
+    if (rc == OCTO_OK && max_items > 0) st->launches += 1;
+    return rc;
 }
 
 extern "C" int octo_stage_status(octo_stage_t* st, uint32_t* status_word, void* cuda_stream) {

@@ -28,6 +28,7 @@ struct octo_stage {
     bool tab_on_device;  // the current batch's table is d_tab (octo_adopt_items_device), not `frames`
     int max_w, max_h;  // largest frame of the batch
     bool have_dets;
+    int cropped_branches;  // bit b: branch b's item table belongs to the current detections
     const octo_det_t* d_dets;
     const int32_t* d_last_n_items[OCTO_MAX_BRANCHES];  // {packed, total} of the last crop call per branch (caller's buffer)
     int64_t launches;
