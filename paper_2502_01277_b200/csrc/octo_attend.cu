@@ -2,7 +2,10 @@
 // few query rows, and the kernel that joins work split over the keys.
 #include <math.h>
 
+#include <type_traits>
+
 #include "octo_attend.cuh"
+#include "octo_attend_tile.h"
 
 namespace octo {
 
@@ -335,7 +338,8 @@ attend_join_kernel(const __grid_constant__ AttendArgs a) {
 // The plan of a call: which kernel, and into how many splits.  It follows from sizes alone.
 // ---------------------------------------------------------------------------------------
 struct AttendPlan {
-    int64_t row_tiles;  // per segment and key head
+    bool tile;            // attend_tile_kernel, else attend_step_kernel
+    int64_t row_tiles;    // per segment and key head
     int splits, chunk;
     int64_t ctas;
     int64_t workspace;
@@ -368,28 +372,37 @@ static int make_plan(const octo_attend_t* c, int sms, AttendPlan* p) {
     const int64_t group = c->heads / c->kv_heads;
     const int64_t max_q = bound_of(c->max_q, c->d_q_offsets, c->q_rows, c->q_total);
     const int64_t max_k = bound_of(c->max_k, c->d_k_offsets, c->k_rows, c->k_total);
-    p->row_tiles = (max_q * group + kStepRows - 1) / kStepRows;
-    if ((double)c->segments * c->kv_heads * (double)p->row_tiles > (double)INT32_MAX) return OCTO_E_CAPACITY;
+    p->tile = max_q * group > kStepRows;
+    const int64_t tile_rows = p->tile ? kTileRows : kStepRows, step = p->tile ? kTileKeys : kStepKeys;
+    p->row_tiles = (max_q * group + tile_rows - 1) / tile_rows;
+    if ((double)c->segments * c->kv_heads * (double)p->row_tiles > (double)INT64_MAX / 1024) return OCTO_E_CAPACITY;
     const int64_t units = (int64_t)c->segments * c->kv_heads * p->row_tiles;
-    const int64_t rows_at_most = (c->q_total * group + kStepRows - 1) / kStepRows + c->segments;
-    const int64_t busy = units < rows_at_most * c->kv_heads ? units : rows_at_most * c->kv_heads;
-    const int64_t want = (int64_t)sms * 12;
-    int64_t splits = busy >= want ? 1 : (want + busy - 1) / busy;
+    // no more tiles than the rows make, with one that is not full in every segment
+    const int64_t rows_make = (c->q_total * group + tile_rows - 1) / tile_rows + c->segments;
+    const int64_t busy = units < rows_make * c->kv_heads ? units : rows_make * c->kv_heads;
+    const int64_t want = p->tile ? sms : (int64_t)sms * 12;
+    int64_t splits = p->tile ? (want / busy < 1 ? 1 : want / busy) : (busy >= want ? 1 : (want + busy - 1) / busy);
     int64_t chunk = (max_k + splits - 1) / splits;
     if (chunk < 512) chunk = 512;
-    chunk = (chunk + kStepKeys - 1) / kStepKeys * kStepKeys;
+    chunk = (chunk + step - 1) / step * step;
     splits = (max_k + chunk - 1) / chunk;
     p->splits = (int)splits;
     p->chunk = splits == 1 ? (int)max_k : (int)chunk;
-    p->ctas = units * splits;
+    p->ctas = p->tile ? (busy * splits < sms ? busy * splits : sms) : units * splits;
     p->workspace = splits == 1 ? 0 : splits * c->q_total * c->heads * (c->head_dim + 2) * (int64_t)sizeof(float);
-    return p->ctas > INT32_MAX || p->workspace < 0 ? OCTO_E_CAPACITY : OCTO_OK;
+    if (p->ctas > INT32_MAX || (!c->d_q_offsets && units > INT32_MAX)) return OCTO_E_CAPACITY;
+    return OCTO_OK;
 }
 
 template <typename T>
 static cudaError_t launch_attend(const AttendArgs& a, const AttendPlan& p, cudaStream_t stream) {
-    auto kernel = a.dim <= 64 ? attend_step_kernel<T, 1> : attend_step_kernel<T, 2>;
-    cudaError_t e = launch_kernel(kernel, dim3((unsigned)p.ctas), dim3(kStepThreads), 0, stream, a, (int)p.row_tiles);
+    cudaError_t e;
+    if (p.tile) {
+        e = launch_attend_tile(a, std::is_same<T, __nv_bfloat16>::value, (int)p.ctas, (int)p.row_tiles, stream);
+    } else {
+        auto kernel = a.dim <= 64 ? attend_step_kernel<T, 1> : attend_step_kernel<T, 2>;
+        e = launch_kernel(kernel, dim3((unsigned)p.ctas), dim3(kStepThreads), 0, stream, a, (int)p.row_tiles);
+    }
     if (e == cudaSuccess && a.splits > 1) {
         const int64_t blocks = (a.q_total * a.heads * 32 + kJoinThreads - 1) / kJoinThreads;
         e = launch_kernel(attend_join_kernel<T>, dim3((unsigned)blocks), dim3(kJoinThreads), 0, stream, a);
@@ -461,6 +474,7 @@ extern "C" int octo_cross_attention(const octo_attend_t* c, void* d_workspace, i
     a.max_k = bound_of(c->max_k, c->d_k_offsets, c->k_rows, c->k_total);
     a.mask = c->d_key_mask;
     a.scale_log2 = (float)((double)c->scale * 1.44269504088896340736);
+    if (a.scale_log2 == 0.0f) a.scale_log2 = 1e-30f;  // equal weights, and still no weight for what is hidden (-infinity)
     a.segments = c->segments;
     a.heads = c->heads;
     a.kv_heads = c->kv_heads;

@@ -1,0 +1,602 @@
+// Attention for many query rows: both products on the tensor cores (tcgen05), accumulators in tensor memory.
+//
+// Work items are tiles of 256 rows -- pairs (query row, head) that share a key head -- of one segment and one split
+// of its keys; a persistent grid of one CTA per SM walks over them.  Inside a CTA
+//   warps 0-3, 4-7   one softmax group per half (128 rows, a thread per row): scores from tensor memory, running
+//                    maximum and sum in registers, weights back into tensor memory over the scores they came from;
+//                    at the end the half's rows of the result.
+//   warp 8           one thread issues all matrix instructions: S_h = Q_h K^T, O_h += P_h V.  The two halves take
+//                    turns, so that one half's softmax runs while the tensor cores work for the other.
+//   warps 9-11       fetch queries, keys and values with 16-byte asynchronous copies into shared memory, in the
+//                    128-byte swizzle that the matrix instructions read.  Copies by row (rather than by tensor
+//                    map) let a tile consist of the VISIBLE keys only, wherever they lie: hidden keys cost a byte
+//                    of mask and nothing else, and what they hold is never looked at.
+// Tensor memory: S0 | S1 | O0 | O1, 128 columns each; the weights, two to a column, overlay the first half of S.
+// A rescaling of O is rare: the reference that the exponents are taken against only follows the row's maximum
+// when it has grown by more than 2^8 (weights up to 2^8 lose nothing in binary32 sums or 16-bit weights), and the
+// group then rescales O itself between the arrival of S (all earlier products have completed) and that of P.
+#include <math.h>
+
+#include "octo_attend.cuh"
+#include "octo_attend_tile.h"
+
+namespace octo {
+
+constexpr int kTileThreads = 384;
+constexpr int kHalf = 128;            // rows of a half, keys of a tile
+constexpr int kLoaders = 96;
+constexpr int kBlockBytes = 128 * 128;  // 128 rows of 64 elements
+constexpr int kListInts = 256;
+constexpr float kSlack = 8.0f;        // growth of the maximum, as a power of two, before the reference follows
+
+template <int DB>
+struct TileShape {
+    static constexpr int kStages = DB == 1 ? 8 : 4;  // 16 or 32 KB each
+    static constexpr int kStageBytes = DB * kBlockBytes;
+    static constexpr int kQBytes = 2 * kStageBytes;
+};
+
+struct TileShared {
+    uint64_t full[8], empty[8];
+    uint64_t q_full, q_empty, done;
+    uint64_t s_full[2], p_full[2], o_full[2], o_empty[2];
+    int meta[16];       // per key tile, by the loaders: visible keys | last << 16
+    int half_meta[2][4];  // the same per half, by the issuing thread
+    uint32_t tmem;
+    int list[3][kListInts];
+};
+
+// ---- tensor core and tensor memory ----------------------------------------------------------------------
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo) {
+    // start address, leading and stride offset in units of 16 bytes; version 1; 128-byte swizzle; 8-row groups of 1024 bytes
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) |
+           (2ull << 61);
+}
+template <typename T> struct MmaFormat;
+template <> struct MmaFormat<__half> { static constexpr uint32_t kCode = 0; };
+template <> struct MmaFormat<__nv_bfloat16> { static constexpr uint32_t kCode = 1; };
+template <typename T>
+__device__ __forceinline__ uint32_t instr_desc(int n, bool b_mn_major) {
+    // binary32 accumulator, both operands of type T, A along K, B along K or along N
+    const uint32_t fmt = MmaFormat<T>::kCode;
+    return (1u << 4) | (fmt << 7) | (fmt << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tmem_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+#define OCTO_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define OCTO_W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+// 32 columns of the warp's 32 lanes; lane l holds row l
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
+        "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : OCTO_R8(r, 0), OCTO_R8(r, 8), OCTO_R8(r, 16), OCTO_R8(r, 24)
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::OCTO_W8(r, 0), OCTO_W8(r, 8), OCTO_W8(r, 16), OCTO_W8(r, 24), "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::OCTO_W8(r, 0),
+        OCTO_W8(r, 8), "r"(addr)
+        : "memory");
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool take) {
+    const uint32_t bytes = take ? 16u : 0u;  // nothing is read, zeros are written
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// ---- work items -------------------------------------------------------------------------------------------
+struct TileItem {
+    Segment seg;
+    int kvh, split, row0, rows;  // first row of the tile and rows in it (1 .. 256)
+    int kb, ke;                  // key rows of this split, inside the segment
+    bool last;                   // the segment's only split: writes the result
+};
+
+// Item w of the grid's list; false where there is nothing to do.  prefix: first tile of every segment (ragged
+// queries), or null: tiles_per_segment each.
+__device__ __forceinline__ bool tile_item(const AttendArgs& a, const int* prefix, int tiles_per_segment, int64_t w, TileItem& it) {
+    it.split = (int)(w % a.splits);
+    const int64_t u = w / a.splits;
+    int s, tiles, first;
+    if (prefix) {
+        int lo = 0, hi = a.segments;  // last s with prefix[s] * kv_heads <= u
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if ((int64_t)prefix[mid] * a.kv_heads <= u) lo = mid; else hi = mid;
+        }
+        s = lo;
+        first = prefix[s];
+        tiles = prefix[s + 1] - first;
+    } else {
+        s = (int)(u / ((int64_t)tiles_per_segment * a.kv_heads));
+        tiles = tiles_per_segment;
+        first = s * tiles_per_segment;
+    }
+    const int in = (int)(u - (int64_t)first * a.kv_heads);
+    it.kvh = in / tiles;
+    it.row0 = (in - it.kvh * tiles) * (2 * kHalf);
+    it.seg = segment_of(a, s);
+    it.rows = min(it.seg.qn * a.group - it.row0, 2 * kHalf);
+    it.kb = min(it.split * a.chunk, it.seg.kn);
+    it.ke = min(it.kb + a.chunk, it.seg.kn);
+    it.last = it.seg.kn <= a.chunk;
+    return it.rows > 0 && (it.split == 0 || it.kb < it.ke);
+}
+
+// One wait of a role.  A wait that runs out is reported; the role then leaves, and so do the others in turn.
+__device__ __forceinline__ bool tile_wait(uint64_t* bar, uint32_t parity, unsigned int* status) {
+    if (mbar_wait_bounded(bar, parity)) return true;
+    if (status) atomicOr(status, OCTO_STATUS_COPY_TIMEOUT);
+    return false;
+}
+
+template <int DB>
+struct Loader {
+    unsigned int* status;
+    int lane, warp;
+    uint32_t slot = 0;             // ring slots issued so far
+    uint64_t *oldest, *second, *newest;  // barriers of the groups in flight
+    int in_flight = 0;
+    bool dead = false;
+
+    __device__ __forceinline__ void arrive_oldest() {
+        fence_proxy_async();  // the matrix instructions read through the asynchronous proxy
+        mbar_arrive(oldest);
+        oldest = second;
+        second = newest;
+        --in_flight;
+    }
+    __device__ __forceinline__ void issued(uint64_t* bar) {
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (in_flight == 0) oldest = bar;
+        else if (in_flight == 1) second = bar;
+        else newest = bar;
+        if (++in_flight == 3) {
+            asm volatile("cp.async.wait_group 2;" ::: "memory");
+            arrive_oldest();
+        }
+    }
+    __device__ __forceinline__ void flush() {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        while (in_flight > 0) arrive_oldest();
+    }
+    // Whoever waits hands over what has landed first: the wait may be for a consumer of just that.
+    __device__ __forceinline__ void wait(uint64_t* bar, uint32_t parity) {
+        if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity, 20u))) return;
+        flush();
+        if (!__all_sync(0xffffffffu, tile_wait(bar, parity, status))) dead = true;
+    }
+
+    static constexpr int kLanesPerRow = 8 * DB, kRowsAtOnce = 32 / kLanesPerRow;
+    // Rows `count` of a tile; row_at(r) gives the row's address (of its first element) or null for zeros.
+    template <typename F>
+    __device__ __forceinline__ void rows(uint32_t dst, int count, int dim_bytes, F row_at) {
+        const int c = lane & (kLanesPerRow - 1);
+        const bool wide = c * 16 < dim_bytes;
+        const uint32_t column = (uint32_t)(c >> 3) * kBlockBytes;
+#pragma unroll 4
+        for (int r = warp * kRowsAtOnce + lane / kLanesPerRow; r < count; r += 3 * kRowsAtOnce) {
+            const char* p = row_at(r);
+            const bool take = wide && p != nullptr;
+            const uint32_t at = dst + column + (uint32_t)(r >> 7) * (DB * kBlockBytes) + (uint32_t)(r & 127) * 128u +
+                                (uint32_t)(((c & 7) ^ (r & 7)) << 4);
+            cp_async16(at, (take ? p : zero_row) + (take ? c * 16 : 0), take);
+        }
+    }
+    const char* zero_row;  // any valid address
+};
+
+template <typename T, int DB>
+__global__ void __launch_bounds__(kTileThreads, 1)
+attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, int ragged) {
+    using Shape = TileShape<DB>;
+    extern __shared__ uint8_t raw[];
+    uint8_t* const base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    TileShared* const sh = reinterpret_cast<TileShared*>(base + Shape::kQBytes + Shape::kStages * Shape::kStageBytes);
+    int* const prefix = ragged ? reinterpret_cast<int*>(sh + 1) : nullptr;
+    const uint32_t q_base = smem_u32(base), ring = q_base + Shape::kQBytes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < Shape::kStages; ++i) {
+            mbar_init(&sh->full[i], kLoaders);
+            mbar_init(&sh->empty[i], 1);
+        }
+        mbar_init(&sh->q_full, kLoaders);
+        mbar_init(&sh->q_empty, 1);
+        mbar_init(&sh->done, 1);
+        for (int h = 0; h < 2; ++h) {
+            mbar_init(&sh->s_full[h], 2);
+            mbar_init(&sh->p_full[h], kHalf);
+            mbar_init(&sh->o_full[h], 1);
+            mbar_init(&sh->o_empty[h], kHalf);
+        }
+        mbar_fence_init();
+    }
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sh->tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    pdl_wait();
+    if (ragged) {
+        for (int s = threadIdx.x; s < a.segments; s += kTileThreads)
+            prefix[s + 1] = (segment_of(a, s).qn * a.group + 2 * kHalf - 1) / (2 * kHalf);
+        __syncthreads();
+        if (warp == 0) {  // inclusive sums, a strip of segments per lane
+            const int strip = (a.segments + 31) >> 5, b = lane * strip, e = min(a.segments, b + strip);
+            int64_t sum = 0;
+            for (int s = b; s < e; ++s) sum += prefix[s + 1];
+            int64_t run = sum;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int64_t t = __shfl_up_sync(0xffffffffu, run, off);
+                if (lane >= off) run += t;
+            }
+            run -= sum;
+            for (int s = b; s < e; ++s) {
+                run += prefix[s + 1];
+                prefix[s + 1] = (int)min(run, (int64_t)1 << 30);  // (more than rows that do not overlap can make)
+            }
+            if (lane == 0) prefix[0] = 0;
+        }
+    }
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    const uint32_t tmem = sh->tmem;
+    const int64_t total = (ragged ? (int64_t)prefix[a.segments] : (int64_t)a.segments * tiles_per_segment) * a.kv_heads * a.splits;
+
+    if (warp < 8) {
+        // ---------------- softmax of one half ----------------
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        const int h = warp >> 2, row = threadIdx.x & (kHalf - 1);
+        const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);  // the warp's 32 lanes of tensor memory
+        const uint32_t s_at = lanes + 128u * h, o_at = lanes + 256u + 128u * h;
+        const float sc = a.scale_log2;
+        const int o_chunks = (a.dim + 31) >> 5;
+        uint32_t tiles = 0, items = 0;
+        bool dead = false;
+        for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
+            TileItem it;
+            if (!tile_item(a, prefix, tiles_per_segment, w, it) || it.rows <= h * kHalf) continue;
+            const int r = it.row0 + h * kHalf + row;
+            const bool real = r < it.row0 + it.rows;
+            float ref = -INFINITY, sum = 0.0f;  // what the exponents are taken against; sum of the weights
+            bool last = false, first = true;
+            while (!last && !dead) {
+                if (!__all_sync(0xffffffffu, tile_wait(&sh->s_full[h], tiles & 1, a.status))) {
+                    dead = true;
+                    break;
+                }
+                tmem_after_sync();
+                const int meta = sh->half_meta[h][tiles & 3], take = meta & 0xffff;
+                ++tiles;
+                last = meta >> 16;
+                uint32_t s[128];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (c == 0 || 32 * c < take) tmem_ld32(s_at + 32 * c, s + 32 * c);
+                tmem_wait_ld();
+                if (take < kHalf) {  // columns behind the last visible key
+                    const uint32_t none = __float_as_uint(sc < 0.0f ? INFINITY : -INFINITY);
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (i >= take) s[i] = none;
+                }
+                float top;
+                if (sc < 0.0f) {
+                    float m[4] = {INFINITY, INFINITY, INFINITY, INFINITY};
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) m[i & 3] = fminf(m[i & 3], __uint_as_float(s[i]));
+                    top = fminf(fminf(m[0], m[1]), fminf(m[2], m[3]));
+                } else {
+                    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) m[i & 3] = fmaxf(m[i & 3], __uint_as_float(s[i]));
+                    top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+                }
+                top = take > 0 ? top * sc : -INFINITY;
+                // (a comparison that is false for NaN leaves the reference; the NaN comes through the exponents)
+                if (__any_sync(0xffffffffu, top > ref + kSlack)) {
+                    const float now = fmaxf(ref, top);
+                    const float f = now == -INFINITY ? 1.0f : ex2(ref - now);
+                    sum *= f;
+                    ref = now;
+                    if (!first) {
+                        for (int c = 0; c < o_chunks; ++c) {
+                            uint32_t o[32];
+                            tmem_ld32(o_at + 32 * c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_st32(o_at + 32 * c, o);
+                        }
+                    }
+                }
+                first = false;
+                const float minus = ref == -INFINITY ? 0.0f : -ref;
+                float part[2] = {0.0f, 0.0f};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if (c > 0 && 32 * c >= take) continue;
+                    uint32_t p[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float x = ex2(fmaf(__uint_as_float(s[32 * c + 2 * i]), sc, minus));
+                        const float y = ex2(fmaf(__uint_as_float(s[32 * c + 2 * i + 1]), sc, minus));
+                        part[0] += x;
+                        part[1] += y;
+                        // the weights in the type of the values: what the matrix instruction takes (the sum keeps them unrounded)
+                        p[i] = pack2<T>(x, y);
+                    }
+                    tmem_st16(s_at + 16 * c, p);
+                }
+                sum += part[0] + part[1];
+                tmem_wait_st();
+                tmem_before_sync();
+                mbar_arrive(&sh->p_full[h]);
+            }
+            // the half's rows of the result
+            if (!dead && !__all_sync(0xffffffffu, tile_wait(&sh->o_full[h], items & 1, a.status))) dead = true;
+            ++items;
+            tmem_after_sync();
+            const int qrow = r / a.group, head = it.kvh * a.group + (r - qrow * a.group);
+            const int64_t part_at = ((int64_t)it.split * a.q_total + it.seg.q0 + qrow) * a.heads + head;
+            T* const out = static_cast<T*>(a.out) + (it.seg.q0 + qrow) * a.o_row + head * a.o_head;
+            if (dead) sum = __int_as_float(0x7fffffff);
+            const float inv = it.last ? (sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f) : 1.0f;
+            for (int c = 0; c < o_chunks; ++c) {
+                uint32_t o[32];
+                __syncwarp();
+                tmem_ld32(o_at + 32 * c, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    const int d = 32 * c + i;
+                    if (!real || d >= a.dim) continue;
+                    float f[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(o[i + j]) * inv;
+                    if (it.last) {
+                        *reinterpret_cast<uint4*>(out + d) =
+                            make_uint4(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]), pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7]));
+                    } else {
+                        float4* const p = reinterpret_cast<float4*>(a.part_o + part_at * a.dim + d);
+                        p[0] = make_float4(f[0], f[1], f[2], f[3]);
+                        p[1] = make_float4(f[4], f[5], f[6], f[7]);
+                    }
+                }
+            }
+            if (real && !it.last) a.part_ml[part_at] = make_float2(dead ? 0.0f : ref, sum);
+            __syncwarp();
+            tmem_before_sync();
+            mbar_arrive(&sh->o_empty[h]);
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        if (warp == 8) {
+            if (lane == 0) {
+                // ---------------- matrix instructions ----------------
+                const int ksteps = (a.dim + 15) >> 4;
+                const uint32_t idesc_pv = instr_desc<T>(16 * ksteps, true);
+                uint32_t slot = 0, tile = 0, items = 0;
+                uint32_t half_tiles[2] = {0, 0}, half_items[2] = {0, 0};
+                bool ok = true;
+                auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && tile_wait(bar, parity, a.status); };
+                auto full_wait = [&](uint32_t n) { wait(&sh->full[n % Shape::kStages], (n / Shape::kStages) & 1); };
+                auto slot_at = [&](uint32_t n) { return ring + (n % Shape::kStages) * Shape::kStageBytes; };
+                auto scores = [&](int h, uint32_t k_slot, int meta) {  // S_h = Q_h K^T over the visible keys
+                    const int n = max(16, ((meta & 0xffff) + 15) & ~15);
+                    const uint32_t idesc = instr_desc<T>(n, false);
+                    for (int k = 0; k < ksteps; ++k) {
+                        const uint32_t off = (uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32u;
+                        mma_ss(tmem + 128u * h, smem_desc(q_base + h * Shape::kStageBytes + off, 16), smem_desc(slot_at(k_slot) + off, 16),
+                               idesc, k > 0);
+                    }
+                    sh->half_meta[h][half_tiles[h] & 3] = meta;
+                    mma_commit(&sh->s_full[h]);
+                    mbar_arrive(&sh->s_full[h]);
+                };
+                for (int64_t w = blockIdx.x; w < total && ok; w += gridDim.x) {
+                    TileItem it;
+                    if (!tile_item(a, prefix, tiles_per_segment, w, it)) continue;
+                    const int halves = it.rows > kHalf ? 2 : 1;
+                    wait(&sh->q_full, items & 1);
+                    full_wait(slot);
+                    if (!ok) break;
+                    tmem_after_sync();
+                    int meta = sh->meta[tile & 15];
+                    for (int h = 0; h < halves; ++h) scores(h, slot, meta);
+                    mma_commit(&sh->empty[slot % Shape::kStages]);
+                    if (meta >> 16) mma_commit(&sh->q_empty);
+                    ++slot;
+                    for (bool first = true;; first = false) {
+                        const bool last = meta >> 16;
+                        const int steps = max(1, ((meta & 0xffff) + 15) >> 4);
+                        int next = 0;
+                        full_wait(slot);
+                        for (int h = 0; h < halves; ++h) {
+                            wait(&sh->p_full[h], half_tiles[h] & 1);
+                            if (first) wait(&sh->o_empty[h], (half_items[h] & 1) ^ 1);
+                            if (!ok) break;
+                            tmem_after_sync();
+                            ++half_tiles[h];
+                            for (int k = 0; k < steps; ++k)
+                                mma_ts(tmem + 256u + 128u * h, tmem + 128u * h + 8u * k, smem_desc(slot_at(slot) + 2048u * k, kBlockBytes),
+                                       idesc_pv, !first || k > 0);
+                            if (last) {
+                                mma_commit(&sh->o_full[h]);
+                                ++half_items[h];
+                            } else {
+                                if (h == 0) {
+                                    full_wait(slot + 1);
+                                    if (!ok) break;
+                                    next = sh->meta[(tile + 1) & 15];
+                                }
+                                scores(h, slot + 1, next);
+                            }
+                        }
+                        if (!ok) break;
+                        mma_commit(&sh->empty[slot % Shape::kStages]);
+                        ++slot;
+                        ++tile;
+                        if (last) break;
+                        mma_commit(&sh->empty[slot % Shape::kStages]);
+                        if (next >> 16) mma_commit(&sh->q_empty);
+                        ++slot;
+                        meta = next;
+                    }
+                    ++items;
+                }
+                mma_commit(&sh->done);  // nothing of this CTA is under way when it gives its memory back
+                tile_wait(&sh->done, 0, a.status);
+            }
+        } else {
+            // ---------------- loads ----------------
+            Loader<DB> ld;
+            ld.status = a.status;
+            ld.lane = lane;
+            ld.warp = warp - 9;
+            ld.zero_row = static_cast<const char*>(a.q);
+            int* const list = sh->list[warp - 9];
+            const int dim_bytes = 2 * a.dim;
+            uint32_t items = 0, tile = 0;
+            for (int64_t w = blockIdx.x; w < total && !ld.dead; w += gridDim.x) {
+                TileItem it;
+                if (!tile_item(a, prefix, tiles_per_segment, w, it)) continue;
+                ld.wait(&sh->q_empty, (items & 1) ^ 1);
+                if (ld.dead) break;
+                const T* const q = static_cast<const T*>(a.q) + it.seg.q0 * a.q_row + (int64_t)it.kvh * a.group * a.q_head;
+                ld.rows(q_base, it.rows > kHalf ? 2 * kHalf : kHalf, dim_bytes, [&](int r) -> const char* {
+                    if (r >= it.rows) return nullptr;
+                    const int vr = it.row0 + r, qrow = vr / a.group;
+                    return reinterpret_cast<const char*>(q + qrow * a.q_row + (vr - qrow * a.group) * a.q_head);
+                });
+                ld.issued(&sh->q_full);
+                ++items;
+                const char* const k = reinterpret_cast<const char*>(static_cast<const T*>(a.k) + it.seg.k0 * a.k_row + it.kvh * a.k_head);
+                const char* const v = reinterpret_cast<const char*>(static_cast<const T*>(a.v) + it.seg.k0 * a.v_row + it.kvh * a.v_head);
+                const uint8_t* const mask = a.mask ? a.mask + it.seg.k0 : nullptr;
+                int cursor = it.kb, listed = 0;
+                for (bool last = false; !last && !ld.dead; ++tile) {
+                    // the next 128 visible keys
+                    int take, from = cursor;
+                    if (mask) {
+                        while (listed <= kHalf && cursor < it.ke) {
+                            bool seen[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const int key = cursor + 32 * j + lane;
+                                seen[j] = key < it.ke && mask[key] != 0;
+                            }
+                            // (at most 128 are listed here, and 128 more fit)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const unsigned ballot = __ballot_sync(0xffffffffu, seen[j]);
+                                if (seen[j]) list[listed + __popc(ballot & ((1u << lane) - 1u))] = cursor + 32 * j + lane;
+                                listed += __popc(ballot);
+                            }
+                            cursor += 128;
+                        }
+                        __syncwarp();
+                        take = min(listed, kHalf);
+                        last = listed <= kHalf;
+                    } else {
+                        take = min(it.ke - cursor, kHalf);
+                        cursor += take;
+                        last = cursor >= it.ke;
+                    }
+                    const int padded = max(16, (take + 15) & ~15);  // rows that the matrix instructions read
+                    if (warp == 9 && lane == 0) sh->meta[tile & 15] = take | (last ? 1 << 16 : 0);
+#pragma unroll
+                    for (int which = 0; which < 2; ++which) {
+                        const uint32_t n = ld.slot;
+                        ld.wait(&sh->empty[n % Shape::kStages], ((n / Shape::kStages) & 1) ^ 1);
+                        if (ld.dead) break;
+                        const char* const src = which ? v : k;
+                        const int64_t stride = 2 * (which ? a.v_row : a.k_row);
+                        const uint32_t dst = ring + (n % Shape::kStages) * Shape::kStageBytes;
+                        if (mask)
+                            ld.rows(dst, padded, dim_bytes, [&](int r) -> const char* { return r < take ? src + list[r] * stride : nullptr; });
+                        else
+                            ld.rows(dst, padded, dim_bytes, [&](int r) -> const char* { return r < take ? src + (from + r) * stride : nullptr; });
+                        ld.issued(&sh->full[n % Shape::kStages]);
+                        ++ld.slot;
+                    }
+                    if (mask) {  // what is left over moves to the front
+                        listed -= take;
+                        int rest[4];
+                        __syncwarp();
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) rest[j] = 32 * j + lane < listed ? list[kHalf + 32 * j + lane] : 0;
+                        __syncwarp();
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (32 * j + lane < listed) list[32 * j + lane] = rest[j];
+                        __syncwarp();
+                    }
+                }
+            }
+            ld.flush();
+        }
+    }
+    tmem_before_sync();
+    __syncthreads();
+    if (warp == 8) {
+        __syncwarp();
+        tmem_after_sync();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    }
+}
+
+template <typename T, int DB>
+static cudaError_t launch_shape(const AttendArgs& a, int grid, int tiles_per_segment, cudaStream_t stream) {
+    using Shape = TileShape<DB>;
+    const bool ragged = a.q_offsets != nullptr;
+    const size_t fixed = 1024 + Shape::kQBytes + Shape::kStages * Shape::kStageBytes + sizeof(TileShared);
+    const size_t most = fixed + sizeof(int) * (OCTO_MAX_SEGMENTS + 1);
+    static_assert(1024 + Shape::kQBytes + Shape::kStages * Shape::kStageBytes + sizeof(TileShared) +
+                          sizeof(int) * (OCTO_MAX_SEGMENTS + 1) <= 232448,
+                  "shared memory of a CTA");
+    auto kernel = attend_tile_kernel<T, DB>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+    if (e != cudaSuccess) return e;
+    const size_t smem = fixed + (ragged ? sizeof(int) * ((size_t)a.segments + 1) : 0);
+    return launch_kernel(kernel, dim3((unsigned)grid), dim3(kTileThreads), smem, stream, a, tiles_per_segment, ragged ? 1 : 0);
+}
+
+cudaError_t launch_attend_tile(const AttendArgs& a, int bf16, int grid, int tiles_per_segment, cudaStream_t stream) {
+    if (a.dim <= 64)
+        return bf16 ? launch_shape<__nv_bfloat16, 1>(a, grid, tiles_per_segment, stream)
+                    : launch_shape<__half, 1>(a, grid, tiles_per_segment, stream);
+    return bf16 ? launch_shape<__nv_bfloat16, 2>(a, grid, tiles_per_segment, stream)
+                : launch_shape<__half, 2>(a, grid, tiles_per_segment, stream);
+}
+
+}  // namespace octo
