@@ -47,10 +47,16 @@ struct TileShared {
 };
 
 // ---- tensor core and tensor memory ----------------------------------------------------------------------
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo) {
-    // start address, leading and stride offset in units of 16 bytes; version 1; 128-byte swizzle; 8-row groups of 1024 bytes
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) |
-           (2ull << 61);
+// Descriptor of a shared-memory operand in the 128-byte swizzle.  Low word: start address and leading offset (distance
+// of 64-element blocks for the values, unused else) in units of 16 bytes; high word: 8-row groups of 1024 bytes,
+// version 1, swizzle mode.  The issuing thread keeps low words and adds to them: one thread issues everything, so
+// a descriptor put together anew for every instruction was what the kernel waited for (145 clocks each).
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t lead) { return ((addr & 0x3ffffu) >> 4) | ((lead >> 4) << 16); }
+__device__ __forceinline__ uint64_t desc_of(uint32_t low) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(low), "r"(kDescHigh));
+    return d;
 }
 template <typename T> struct MmaFormat;
 template <> struct MmaFormat<__half> { static constexpr uint32_t kCode = 0; };
@@ -188,25 +194,50 @@ struct Loader {
     }
     // Whoever waits hands over what has landed first: the wait may be for a consumer of just that.
     __device__ __forceinline__ void wait(uint64_t* bar, uint32_t parity) {
-        if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity, 20u))) return;
+        if (__all_sync(0xffffffffu, mbar_test_wait(bar, parity))) return;
         flush();
         if (!__all_sync(0xffffffffu, tile_wait(bar, parity, status))) dead = true;
     }
 
-    static constexpr int kLanesPerRow = 8 * DB, kRowsAtOnce = 32 / kLanesPerRow;
-    // Rows `count` of a tile; row_at(r) gives the row's address (of its first element) or null for zeros.
+    // A warp takes every third group of 8 rows, kRowsAtOnce rows per instruction; the swizzle of a lane's row inside
+    // its group, and so its place in shared memory, is the same for every group.
+    static constexpr int kLanesPerRow = 8 * DB, kRowsAtOnce = 32 / kLanesPerRow, kTurns = 8 / kRowsAtOnce;
+    uint32_t place[kTurns];  // of the lane's piece of row kRowsAtOnce * i + its own in a group
+    bool wide;               // the lane's piece lies inside the head
+    __device__ __forceinline__ void layout(int dim_bytes) {
+        const int c = lane & (kLanesPerRow - 1), own = lane / kLanesPerRow;
+        wide = c * 16 < dim_bytes;
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const int r = kRowsAtOnce * i + own;
+            place[i] = (uint32_t)(c >> 3) * kBlockBytes + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ r) << 4);
+        }
+    }
+    // Rows [0, count) of a tile, count a multiple of 8; row_at(r) gives a row's address or null for zeros.
     template <typename F>
-    __device__ __forceinline__ void rows(uint32_t dst, int count, int dim_bytes, F row_at) {
-        const int c = lane & (kLanesPerRow - 1);
-        const bool wide = c * 16 < dim_bytes;
-        const uint32_t column = (uint32_t)(c >> 3) * kBlockBytes;
-#pragma unroll 4
-        for (int r = warp * kRowsAtOnce + lane / kLanesPerRow; r < count; r += 3 * kRowsAtOnce) {
-            const char* p = row_at(r);
-            const bool take = wide && p != nullptr;
-            const uint32_t at = dst + column + (uint32_t)(r >> 7) * (DB * kBlockBytes) + (uint32_t)(r & 127) * 128u +
-                                (uint32_t)(((c & 7) ^ (r & 7)) << 4);
-            cp_async16(at, (take ? p : zero_row) + (take ? c * 16 : 0), take);
+    __device__ __forceinline__ void rows(uint32_t dst, int count, F row_at) {
+        const int c = lane & (kLanesPerRow - 1), own = lane / kLanesPerRow;
+        for (int g = warp; g < (count >> 3); g += 3) {
+            const uint32_t at = dst + (uint32_t)(g >> 4) * (DB * kBlockBytes) + (uint32_t)(g & 15) * 1024u;
+#pragma unroll
+            for (int i = 0; i < kTurns; ++i) {
+                const char* p = row_at(8 * g + kRowsAtOnce * i + own);
+                const bool take = wide && p != nullptr;
+                cp_async16(at + place[i], take ? p + c * 16 : zero_row, take);
+            }
+        }
+    }
+    // 128 rows that lie side by side from `src` on, `stride` bytes apart.
+    __device__ __forceinline__ void full_rows(uint32_t dst, const char* src, int64_t stride) {
+        const int c = lane & (kLanesPerRow - 1), own = lane / kLanesPerRow;
+        const char* p = wide ? src + (8 * warp + own) * stride + c * 16 : zero_row;
+        const int64_t turn = wide ? kRowsAtOnce * stride : 0, group = wide ? 24 * stride : 0;
+        uint32_t at = dst + (uint32_t)warp * 1024u;
+        for (int g = warp; g < 16; g += 3) {
+#pragma unroll
+            for (int i = 0; i < kTurns; ++i) cp_async16(at + place[i], p + i * turn, wide);
+            p += group;
+            at += 3 * 1024u;
         }
     }
     const char* zero_row;  // any valid address
@@ -221,7 +252,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
     TileShared* const sh = reinterpret_cast<TileShared*>(base + Shape::kQBytes + Shape::kStages * Shape::kStageBytes);
     int* const prefix = ragged ? reinterpret_cast<int*>(sh + 1) : nullptr;
     const uint32_t q_base = smem_u32(base), ring = q_base + Shape::kQBytes;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < Shape::kStages; ++i) {
@@ -269,12 +300,12 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
     tmem_before_sync();
     __syncthreads();
     tmem_after_sync();
-    const uint32_t tmem = sh->tmem;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, sh->tmem, 0);
     const int64_t total = (ragged ? (int64_t)prefix[a.segments] : (int64_t)a.segments * tiles_per_segment) * a.kv_heads * a.splits;
 
     if (warp < 8) {
         // ---------------- softmax of one half ----------------
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const int h = warp >> 2, row = threadIdx.x & (kHalf - 1);
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);  // the warp's 32 lanes of tensor memory
         const uint32_t s_at = lanes + 128u * h, o_at = lanes + 256u + 128u * h;
@@ -399,29 +430,40 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
             mbar_arrive(&sh->o_empty[h]);
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
         if (warp == 8) {
-            if (lane == 0) {
+            {
                 // ---------------- matrix instructions ----------------
+                // The whole warp walks through the loop and one elected lane issues, so that descriptors and addresses
+                // are the warp's and stay in uniform registers.
                 const int ksteps = (a.dim + 15) >> 4;
-                const uint32_t idesc_pv = instr_desc<T>(16 * ksteps, true);
+                const uint32_t idesc_pv = instr_desc<T>(16 * ksteps, true), idesc_qk = instr_desc<T>(0, false);
                 uint32_t slot = 0, tile = 0, items = 0;
                 uint32_t half_tiles[2] = {0, 0}, half_items[2] = {0, 0};
                 bool ok = true;
-                auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && tile_wait(bar, parity, a.status); };
+                auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, tile_wait(bar, parity, a.status)); };
+                auto commit = [&](uint64_t* bar) {
+                    if (elect_one()) mma_commit(bar);
+                    __syncwarp();
+                };
+                auto meta_at = [&](uint32_t n) { return __shfl_sync(0xffffffffu, sh->meta[n & 15], 0); };
                 auto full_wait = [&](uint32_t n) { wait(&sh->full[n % Shape::kStages], (n / Shape::kStages) & 1); };
                 auto slot_at = [&](uint32_t n) { return ring + (n % Shape::kStages) * Shape::kStageBytes; };
                 auto scores = [&](int h, uint32_t k_slot, int meta) {  // S_h = Q_h K^T over the visible keys
                     const int n = max(16, ((meta & 0xffff) + 15) & ~15);
-                    const uint32_t idesc = instr_desc<T>(n, false);
-                    for (int k = 0; k < ksteps; ++k) {
-                        const uint32_t off = (uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32u;
-                        mma_ss(tmem + 128u * h, smem_desc(q_base + h * Shape::kStageBytes + off, 16), smem_desc(slot_at(k_slot) + off, 16),
-                               idesc, k > 0);
+                    const uint32_t idesc = idesc_qk + ((uint32_t)(n >> 3) << 17);
+                    const uint32_t qa = desc_low(q_base + h * Shape::kStageBytes, 0), ka = desc_low(slot_at(k_slot), 0);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < 4 * DB; ++k) {
+                            const uint32_t off = ((uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32u) >> 4;
+                            if (k < ksteps) mma_ss(tmem + 128u * h, desc_of(qa + off), desc_of(ka + off), idesc, k > 0);
+                        }
+                        sh->half_meta[h][half_tiles[h] & 3] = meta;
+                        mma_commit(&sh->s_full[h]);
+                        mbar_arrive(&sh->s_full[h]);
                     }
-                    sh->half_meta[h][half_tiles[h] & 3] = meta;
-                    mma_commit(&sh->s_full[h]);
-                    mbar_arrive(&sh->s_full[h]);
+                    __syncwarp();
                 };
                 for (int64_t w = blockIdx.x; w < total && ok; w += gridDim.x) {
                     TileItem it;
@@ -431,10 +473,10 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                     full_wait(slot);
                     if (!ok) break;
                     tmem_after_sync();
-                    int meta = sh->meta[tile & 15];
+                    int meta = meta_at(tile);
                     for (int h = 0; h < halves; ++h) scores(h, slot, meta);
-                    mma_commit(&sh->empty[slot % Shape::kStages]);
-                    if (meta >> 16) mma_commit(&sh->q_empty);
+                    commit(&sh->empty[slot % Shape::kStages]);
+                    if (meta >> 16) commit(&sh->q_empty);
                     ++slot;
                     for (bool first = true;; first = false) {
                         const bool last = meta >> 16;
@@ -447,34 +489,40 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                             if (!ok) break;
                             tmem_after_sync();
                             ++half_tiles[h];
-                            for (int k = 0; k < steps; ++k)
-                                mma_ts(tmem + 256u + 128u * h, tmem + 128u * h + 8u * k, smem_desc(slot_at(slot) + 2048u * k, kBlockBytes),
-                                       idesc_pv, !first || k > 0);
+                            const uint32_t va = desc_low(slot_at(slot), kBlockBytes);
+                            if (elect_one()) {
+#pragma unroll
+                                for (int k = 0; k < 8; ++k)
+                                    if (k < steps)
+                                        mma_ts(tmem + 256u + 128u * h, tmem + 128u * h + 8u * k, desc_of(va + 128u * k), idesc_pv,
+                                               !first || k > 0);
+                                if (last) mma_commit(&sh->o_full[h]);
+                            }
+                            __syncwarp();
                             if (last) {
-                                mma_commit(&sh->o_full[h]);
                                 ++half_items[h];
                             } else {
                                 if (h == 0) {
                                     full_wait(slot + 1);
                                     if (!ok) break;
-                                    next = sh->meta[(tile + 1) & 15];
+                                    next = meta_at(tile + 1);
                                 }
                                 scores(h, slot + 1, next);
                             }
                         }
                         if (!ok) break;
-                        mma_commit(&sh->empty[slot % Shape::kStages]);
+                        commit(&sh->empty[slot % Shape::kStages]);
                         ++slot;
                         ++tile;
                         if (last) break;
-                        mma_commit(&sh->empty[slot % Shape::kStages]);
-                        if (next >> 16) mma_commit(&sh->q_empty);
+                        commit(&sh->empty[slot % Shape::kStages]);
+                        if (next >> 16) commit(&sh->q_empty);
                         ++slot;
                         meta = next;
                     }
                     ++items;
                 }
-                mma_commit(&sh->done);  // nothing of this CTA is under way when it gives its memory back
+                commit(&sh->done);  // nothing of this CTA is under way when it gives its memory back
                 tile_wait(&sh->done, 0, a.status);
             }
         } else {
@@ -485,7 +533,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
             ld.warp = warp - 9;
             ld.zero_row = static_cast<const char*>(a.q);
             int* const list = sh->list[warp - 9];
-            const int dim_bytes = 2 * a.dim;
+            ld.layout(2 * a.dim);
             uint32_t items = 0, tile = 0;
             for (int64_t w = blockIdx.x; w < total && !ld.dead; w += gridDim.x) {
                 TileItem it;
@@ -493,7 +541,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                 ld.wait(&sh->q_empty, (items & 1) ^ 1);
                 if (ld.dead) break;
                 const T* const q = static_cast<const T*>(a.q) + it.seg.q0 * a.q_row + (int64_t)it.kvh * a.group * a.q_head;
-                ld.rows(q_base, it.rows > kHalf ? 2 * kHalf : kHalf, dim_bytes, [&](int r) -> const char* {
+                ld.rows(q_base, it.rows > kHalf ? 2 * kHalf : kHalf, [&](int r) -> const char* {
                     if (r >= it.rows) return nullptr;
                     const int vr = it.row0 + r, qrow = vr / a.group;
                     return reinterpret_cast<const char*>(q + qrow * a.q_row + (vr - qrow * a.group) * a.q_head);
@@ -543,9 +591,11 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                         const int64_t stride = 2 * (which ? a.v_row : a.k_row);
                         const uint32_t dst = ring + (n % Shape::kStages) * Shape::kStageBytes;
                         if (mask)
-                            ld.rows(dst, padded, dim_bytes, [&](int r) -> const char* { return r < take ? src + list[r] * stride : nullptr; });
+                            ld.rows(dst, padded, [&](int r) -> const char* { return r < take ? src + list[r] * stride : nullptr; });
+                        else if (take == kHalf)
+                            ld.full_rows(dst, src + from * stride, stride);
                         else
-                            ld.rows(dst, padded, dim_bytes, [&](int r) -> const char* { return r < take ? src + (from + r) * stride : nullptr; });
+                            ld.rows(dst, padded, [&](int r) -> const char* { return r < take ? src + (from + r) * stride : nullptr; });
                         ld.issued(&sh->full[n % Shape::kStages]);
                         ++ld.slot;
                     }
