@@ -569,7 +569,7 @@ typedef struct {
                                       /* concerned become NaN) if a bounded wait of the kernel gives up    */
 } octo_attend_t;
 
-#define OCTO_MAX_SEGMENTS 4096
+#define OCTO_MAX_SEGMENTS 2048
 
 /* Bytes of workspace that octo_cross_attention needs for these arguments (pointers are not looked at); 0 where
  * no work is split over the keys. */

@@ -45,7 +45,7 @@ OCTO_HEAD_PLANES = 1
 OCTO_F16 = 0
 OCTO_BF16 = 1
 OCTO_F32 = 2
-OCTO_MAX_SEGMENTS = 4096
+OCTO_MAX_SEGMENTS = 2048
 HEAD_LAYOUTS = {"rows": OCTO_HEAD_ROWS, "planes": OCTO_HEAD_PLANES}
 
 EXPORTS = (

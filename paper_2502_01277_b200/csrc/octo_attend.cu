@@ -479,6 +479,7 @@ extern "C" int octo_cross_attention(const octo_attend_t* c, void* d_workspace, i
     a.heads = c->heads;
     a.kv_heads = c->kv_heads;
     a.group = c->heads / c->kv_heads;
+    a.group_div.set((unsigned)a.group);
     a.dim = c->head_dim;
     a.splits = p.splits;
     a.chunk = p.chunk;

@@ -8,6 +8,18 @@
 
 namespace octo {
 
+// Division by a number that is the same for a whole launch: exact for 0 <= n < 2^31 (multiply by the reciprocal rounded
+// up to 33 bits, whose top bit is the addition of n).
+struct FastDiv {
+    unsigned mul, shift;
+    void set(unsigned d) {
+        shift = 0;
+        while ((1ull << shift) < d) ++shift;
+        mul = (unsigned)(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
+    }
+    __device__ __forceinline__ int div(int n) const { return (int)((__umulhi(mul, (unsigned)n) + (unsigned)n) >> shift); }
+};
+
 struct AttendArgs {
     const void *q, *k, *v;
     void* out;
@@ -18,6 +30,7 @@ struct AttendArgs {
     const uint8_t* mask;
     float scale_log2;  // scale * log2(e): the softmax is taken to base 2
     int segments, heads, kv_heads, group, dim;
+    FastDiv group_div;
     // Work split over the keys: split i of a segment takes its key rows [i * chunk, (i + 1) * chunk).  A
     // segment of at most `chunk` keys has one active split, which writes the result itself; those of more
     // leave (unnormalised sum, reference maximum, sum of weights) of every row for the joining kernel.

@@ -5,16 +5,17 @@
 //   warps 0-3, 4-7   one softmax group per half (128 rows, a thread per row): scores from tensor memory, running
 //                    maximum and sum in registers, weights back into tensor memory over the scores they came from;
 //                    at the end the half's rows of the result.
-//   warp 8           one thread issues all matrix instructions: S_h = Q_h K^T, O_h += P_h V.  The two halves take
-//                    turns, so that one half's softmax runs while the tensor cores work for the other.
+//   warp 8           issues all matrix instructions: S_h = Q_h K^T, O_h += P_h V.
 //   warps 9-11       fetch queries, keys and values with 16-byte asynchronous copies into shared memory, in the
 //                    128-byte swizzle that the matrix instructions read.  Copies by row (rather than by tensor
 //                    map) let a tile consist of the VISIBLE keys only, wherever they lie: hidden keys cost a byte
 //                    of mask and nothing else, and what they hold is never looked at.
-// Tensor memory: S0 | S1 | O0 | O1, 128 columns each; the weights, two to a column, overlay the first half of S.
+// Keys are fetched 128 at a time and worked on 64 at a time: tensor memory holds two score buffers per half (S0a S0b
+// S1a S1b, 64 columns each, then O0 and O1, 128 each), so that the scores of the next 64 keys are made while the
+// softmax works on these and a half never waits for the matrix instructions of its own weights.
 // A rescaling of O is rare: the reference that the exponents are taken against only follows the row's maximum
-// when it has grown by more than 2^8 (weights up to 2^8 lose nothing in binary32 sums or 16-bit weights), and the
-// group then rescales O itself between the arrival of S (all earlier products have completed) and that of P.
+// when it has grown by more than 2^8 (weights up to 2^8 lose nothing in binary32 sums or 16-bit weights); the
+// group then waits for the products under way and rescales O itself.
 #include <math.h>
 
 #include "octo_attend.cuh"
@@ -24,6 +25,7 @@ namespace octo {
 
 constexpr int kTileThreads = 384;
 constexpr int kHalf = 128;            // rows of a half, keys of a tile
+constexpr int kSub = 64;              // keys of a turn
 constexpr int kLoaders = 96;
 constexpr int kBlockBytes = 128 * 128;  // 128 rows of 64 elements
 constexpr int kListInts = 256;
@@ -36,15 +38,24 @@ struct TileShape {
     static constexpr int kQBytes = 2 * kStageBytes;
 };
 
+// What the other roles need to know of an item, left by the loaders.
+struct TileInfo {
+    int64_t q0, work;       // first query row of the segment; number of the item
+    int kvh, split, row0, rows, last;
+};
+
 struct TileShared {
     uint64_t full[8], empty[8];
     uint64_t q_full, q_empty, done;
-    uint64_t s_full[2], p_full[2], o_full[2], o_empty[2];
-    int meta[16];       // per key tile, by the loaders: visible keys | last << 16
-    int half_meta[2][4];  // the same per half, by the issuing thread
+    uint64_t s_full[2][2], p_full[2][2], pv_done[2], o_empty[2];
+    int meta[16];         // per key tile, by the loaders: visible keys | last << 16
+    int half_meta[2][4];  // per half and turn, by the issuing warp: keys | kLast | item << kItemShift | kStop
+    TileInfo info[4];
     uint32_t tmem;
     int list[3][kListInts];
+    uint4 stage[8][32 * 4];  // per softmax warp: 32 rows of 32 elements on their way out
 };
+constexpr int kLast = 1 << 8, kStop = 1 << 9, kItemShift = 16;
 
 // ---- tensor core and tensor memory ----------------------------------------------------------------------
 // Descriptor of a shared-memory operand in the 128-byte swizzle.  Low word: start address and leading offset (distance
@@ -84,10 +95,10 @@ __device__ __forceinline__ void mma_commit(uint64_t* bar) {
 }
 __device__ __forceinline__ void tmem_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 #define OCTO_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define OCTO_P8(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
 #define OCTO_W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
 // 32 columns of the warp's 32 lanes; lane l holds row l
 __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* r) {
@@ -98,17 +109,21 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* r) {
         : "r"(addr)
         : "memory");
 }
+// The 32 registers of the latest load are there from here on (they pass through, so that no use moves above).
+__device__ __forceinline__ void tmem_landed(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : OCTO_P8(r, 0), OCTO_P8(r, 8), OCTO_P8(r, 16), OCTO_P8(r, 24)::"memory");
+}
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
         "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::OCTO_W8(r, 0), OCTO_W8(r, 8), OCTO_W8(r, 16), OCTO_W8(r, 24), "r"(addr)
         : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::OCTO_W8(r, 0),
-        OCTO_W8(r, 8), "r"(addr)
-        : "memory");
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool take) {
@@ -153,6 +168,12 @@ __device__ __forceinline__ bool tile_item(const AttendArgs& a, const int* prefix
     it.ke = min(it.kb + a.chunk, it.seg.kn);
     it.last = it.seg.kn <= a.chunk;
     return it.rows > 0 && (it.split == 0 || it.kb < it.ke);
+}
+
+// Row r (of a segment and key head) -> query row and head.
+__device__ __forceinline__ void tile_row(const AttendArgs& a, int kvh, int r, int& qrow, int& head) {
+    qrow = a.group_div.div(r);
+    head = kvh * a.group + (r - qrow * a.group);
 }
 
 // One wait of a role.  A wait that runs out is reported; the role then leaves, and so do the others in turn.
@@ -218,7 +239,7 @@ struct Loader {
     __device__ __forceinline__ void rows(uint32_t dst, int count, F row_at) {
         const int c = lane & (kLanesPerRow - 1), own = lane / kLanesPerRow;
         for (int g = warp; g < (count >> 3); g += 3) {
-            const uint32_t at = dst + (uint32_t)(g >> 4) * (DB * kBlockBytes) + (uint32_t)(g & 15) * 1024u;
+            const uint32_t at = dst + (uint32_t)g * 1024u;
 #pragma unroll
             for (int i = 0; i < kTurns; ++i) {
                 const char* p = row_at(8 * g + kRowsAtOnce * i + own);
@@ -263,9 +284,11 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
         mbar_init(&sh->q_empty, 1);
         mbar_init(&sh->done, 1);
         for (int h = 0; h < 2; ++h) {
-            mbar_init(&sh->s_full[h], 2);
-            mbar_init(&sh->p_full[h], kHalf);
-            mbar_init(&sh->o_full[h], 1);
+            mbar_init(&sh->s_full[h][0], 2);
+            mbar_init(&sh->s_full[h][1], 2);
+            mbar_init(&sh->p_full[h][0], kHalf);
+            mbar_init(&sh->p_full[h][1], kHalf);
+            mbar_init(&sh->pv_done[h], 1);
             mbar_init(&sh->o_empty[h], kHalf);
         }
         mbar_fence_init();
@@ -308,126 +331,197 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const int h = warp >> 2, row = threadIdx.x & (kHalf - 1);
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);  // the warp's 32 lanes of tensor memory
-        const uint32_t s_at = lanes + 128u * h, o_at = lanes + 256u + 128u * h;
+        const uint32_t o_at = lanes + 256u + 128u * h;
         const float sc = a.scale_log2;
         const int o_chunks = (a.dim + 31) >> 5;
-        uint32_t tiles = 0, items = 0;
+        uint32_t turn = 0;  // turns so far; the scores of turn n are in buffer n & 1
+        int64_t done_work = -1;
         bool dead = false;
-        for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
-            TileItem it;
-            if (!tile_item(a, prefix, tiles_per_segment, w, it) || it.rows <= h * kHalf) continue;
-            const int r = it.row0 + h * kHalf + row;
-            const bool real = r < it.row0 + it.rows;
+        for (;;) {
             float ref = -INFINITY, sum = 0.0f;  // what the exponents are taken against; sum of the weights
-            bool last = false, first = true;
-            while (!last && !dead) {
-                if (!__all_sync(0xffffffffu, tile_wait(&sh->s_full[h], tiles & 1, a.status))) {
+            bool first = true;
+            int meta = 0;
+            while (!(meta & (kLast | kStop))) {
+                if (!__all_sync(0xffffffffu, tile_wait(&sh->s_full[h][turn & 1], (turn >> 1) & 1, a.status))) {
                     dead = true;
                     break;
                 }
                 tmem_after_sync();
-                const int meta = sh->half_meta[h][tiles & 3], take = meta & 0xffff;
-                ++tiles;
-                last = meta >> 16;
-                uint32_t s[128];
+                meta = sh->half_meta[h][turn & 3];
+                if (meta & kStop) break;
+                const int take = meta & 0xff;
+                const uint32_t s_at = lanes + 128u * h + 64u * (turn & 1);
+                // Weights against the reference so far, and the scores' maximum beside them: the exponentials do not wait
+                // for the maximum.  Only if a row's has outgrown the reference (and for the first turn, whose
+                // scores are looked through before) is the reference moved and the turn, still in tensor memory, taken again.
+                uint32_t p[32];
+                unsigned long long part = 0ull;
+                for (bool look = first;;) {
+                    if (look) {
+                        float top = -INFINITY;
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (c == 0 || 32 * c < take) tmem_ld32(s_at + 32 * c, s + 32 * c);
-                tmem_wait_ld();
-                if (take < kHalf) {  // columns behind the last visible key
-                    const uint32_t none = __float_as_uint(sc < 0.0f ? INFINITY : -INFINITY);
+                        for (int c = 0; c < 2; ++c) {
+                            if (32 * c >= take) break;
+                            uint32_t s[32];
+                            tmem_ld32(s_at + 32 * c, s);
+                            tmem_landed(s);
 #pragma unroll
-                    for (int i = 0; i < 128; ++i)
-                        if (i >= take) s[i] = none;
-                }
-                float top;
-                if (sc < 0.0f) {
-                    float m[4] = {INFINITY, INFINITY, INFINITY, INFINITY};
+                            for (int i = 0; i < 32; ++i)
+                                if (32 * c + i < take) top = fmaxf(top, __uint_as_float(s[i]) * sc);
+                        }
+                        const float now = fmaxf(ref, top);
+                        const float f = now == -INFINITY ? 1.0f : ex2(ref - now);
+                        sum *= f;
+                        ref = now;
+                        if (!first) {  // (of the products, all but the last turn's are complete: the scores came after them)
+                            if (!__all_sync(0xffffffffu, tile_wait(&sh->pv_done[h], (turn - 1) & 1, a.status))) dead = true;
+                            tmem_after_sync();
+                            for (int c = 0; c < o_chunks; ++c) {
+                                uint32_t o[32];
+                                tmem_ld32(o_at + 32 * c, o);
+                                tmem_landed(o);
 #pragma unroll
-                    for (int i = 0; i < 128; ++i) m[i & 3] = fminf(m[i & 3], __uint_as_float(s[i]));
-                    top = fminf(fminf(m[0], m[1]), fminf(m[2], m[3]));
-                } else {
-                    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int i = 0; i < 128; ++i) m[i & 3] = fmaxf(m[i & 3], __uint_as_float(s[i]));
-                    top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-                }
-                top = take > 0 ? top * sc : -INFINITY;
-                // (a comparison that is false for NaN leaves the reference; the NaN comes through the exponents)
-                if (__any_sync(0xffffffffu, top > ref + kSlack)) {
-                    const float now = fmaxf(ref, top);
-                    const float f = now == -INFINITY ? 1.0f : ex2(ref - now);
-                    sum *= f;
-                    ref = now;
-                    if (!first) {
-                        for (int c = 0; c < o_chunks; ++c) {
-                            uint32_t o[32];
-                            tmem_ld32(o_at + 32 * c, o);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            tmem_st32(o_at + 32 * c, o);
+                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                tmem_st32(o_at + 32 * c, o);
+                            }
                         }
                     }
+                    const float minus = ref == -INFINITY ? 0.0f : -ref;
+                    const unsigned long long sc2 = f32x2(sc, sc), minus2 = f32x2(minus, minus);
+                    float top = -INFINITY;  // above the reference
+                    part = 0ull;
+                    uint32_t s[2][32];
+                    tmem_ld32(s_at, s[0]);
+                    tmem_landed(s[0]);
+                    if (take > 32) tmem_ld32(s_at + 32, s[1]);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        if (c > 0) {
+                            if (take <= 32) {  // (the matrix instruction reads the first 32 weights then)
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) p[16 + i] = 0u;
+                                break;
+                            }
+                            tmem_landed(s[1]);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const uint32_t* const in = s[c] + 2 * i;
+                            float x, y;
+                            asm("mov.b64 {%0, %1}, %2;"
+                                : "=f"(x), "=f"(y)
+                                : "l"(fma_f32x2(f32x2(__uint_as_float(in[0]), __uint_as_float(in[1])), sc2, minus2)));
+                            if (take < kSub) {  // columns behind the last visible key
+                                if (32 * c + 2 * i >= take) x = -INFINITY;
+                                if (32 * c + 2 * i + 1 >= take) y = -INFINITY;
+                            }
+                            top = max3(top, x, y);
+                            x = ex2(x);
+                            y = ex2(y);
+                            part = add_f32x2(part, f32x2(x, y));
+                            // the weights in the type of the values: what the matrix instruction takes (the sum keeps them unrounded)
+                            p[16 * c + i] = pack2<T>(x, y);
+                        }
+                    }
+                    // (false for NaN: it leaves the reference and comes through the exponentials)
+                    if (look || !__any_sync(0xffffffffu, (ref == -INFINITY && top > -INFINITY) || top > kSlack)) break;
+                    look = true;
                 }
                 first = false;
-                const float minus = ref == -INFINITY ? 0.0f : -ref;
-                float part[2] = {0.0f, 0.0f};
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    if (c > 0 && 32 * c >= take) continue;
-                    uint32_t p[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float x = ex2(fmaf(__uint_as_float(s[32 * c + 2 * i]), sc, minus));
-                        const float y = ex2(fmaf(__uint_as_float(s[32 * c + 2 * i + 1]), sc, minus));
-                        part[0] += x;
-                        part[1] += y;
-                        // the weights in the type of the values: what the matrix instruction takes (the sum keeps them unrounded)
-                        p[i] = pack2<T>(x, y);
-                    }
-                    tmem_st16(s_at + 16 * c, p);
+                tmem_st32(s_at, p);
+                {
+                    float x, y;
+                    asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(part));
+                    sum += x + y;
                 }
-                sum += part[0] + part[1];
                 tmem_wait_st();
                 tmem_before_sync();
-                mbar_arrive(&sh->p_full[h]);
+                mbar_arrive(&sh->p_full[h][turn & 1]);
+                ++turn;
             }
+            if (dead || (meta & kStop)) break;
             // the half's rows of the result
-            if (!dead && !__all_sync(0xffffffffu, tile_wait(&sh->o_full[h], items & 1, a.status))) dead = true;
-            ++items;
+            const TileInfo it = sh->info[meta >> kItemShift];
+            // the products of the last turn; those of the turn before may still be under way, and their phase comes first
+            if (!__all_sync(0xffffffffu, tile_wait(&sh->pv_done[h], turn & 1, a.status) &&
+                                             tile_wait(&sh->pv_done[h], (turn - 1) & 1, a.status))) {
+                dead = true;
+                break;
+            }
             tmem_after_sync();
-            const int qrow = r / a.group, head = it.kvh * a.group + (r - qrow * a.group);
-            const int64_t part_at = ((int64_t)it.split * a.q_total + it.seg.q0 + qrow) * a.heads + head;
-            T* const out = static_cast<T*>(a.out) + (it.seg.q0 + qrow) * a.o_row + head * a.o_head;
-            if (dead) sum = __int_as_float(0x7fffffff);
+            done_work = it.work;
+            const int r0 = it.row0 + h * kHalf, end = it.row0 + it.rows;
             const float inv = it.last ? (sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f) : 1.0f;
-            for (int c = 0; c < o_chunks; ++c) {
-                uint32_t o[32];
-                __syncwarp();
-                tmem_ld32(o_at + 32 * c, o);
-                tmem_wait_ld();
+            if (it.last) {
+                // four lanes to a row and 64 bytes of it at once, by way of shared memory
+                uint4* const stage = sh->stage[warp];
+                T* row_out[4];
+                bool real[4];
 #pragma unroll
-                for (int i = 0; i < 32; i += 8) {
-                    const int d = 32 * c + i;
-                    if (!real || d >= a.dim) continue;
-                    float f[8];
+                for (int k = 0; k < 4; ++k) {
+                    const int r = r0 + (row & ~31) + 8 * k + (lane >> 2);
+                    int qrow, head;
+                    tile_row(a, it.kvh, r, qrow, head);
+                    real[k] = r < end;
+                    row_out[k] = static_cast<T*>(a.out) + (it.q0 + qrow) * a.o_row + head * a.o_head + 8 * (lane & 3);
+                }
+                for (int c = 0; c < o_chunks; ++c) {
+                    uint32_t o[32];
+                    tmem_ld32(o_at + 32 * c, o);
+                    tmem_landed(o);
+                    __syncwarp();
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(o[i + j]) * inv;
-                    if (it.last) {
-                        *reinterpret_cast<uint4*>(out + d) =
-                            make_uint4(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]), pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7]));
-                    } else {
-                        float4* const p = reinterpret_cast<float4*>(a.part_o + part_at * a.dim + d);
-                        p[0] = make_float4(f[0], f[1], f[2], f[3]);
-                        p[1] = make_float4(f[4], f[5], f[6], f[7]);
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t y[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            y[j] = pack2<T>(__uint_as_float(o[8 * i + 2 * j]) * inv, __uint_as_float(o[8 * i + 2 * j + 1]) * inv);
+                        stage[4 * lane + (i ^ ((lane >> 1) & 3))] = make_uint4(y[0], y[1], y[2], y[3]);
+                    }
+                    __syncwarp();
+                    const bool inside = 32 * c + 8 * (lane & 3) < a.dim;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int l = 8 * k + (lane >> 2);
+                        const uint4 v = stage[4 * l + ((lane & 3) ^ ((l >> 1) & 3))];
+                        if (real[k] && inside) *reinterpret_cast<uint4*>(row_out[k] + 32 * c) = v;
                     }
                 }
+            } else {
+                const int r = r0 + row;
+                int qrow, head;
+                tile_row(a, it.kvh, r, qrow, head);
+                const int64_t at = ((int64_t)it.split * a.q_total + it.q0 + qrow) * a.heads + head;
+                for (int c = 0; c < o_chunks; ++c) {
+                    uint32_t o[32];
+                    __syncwarp();
+                    tmem_ld32(o_at + 32 * c, o);
+                    tmem_landed(o);
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4)
+                        if (r < end && 32 * c + i < a.dim)
+                            *reinterpret_cast<uint4*>(a.part_o + at * a.dim + 32 * c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                }
+                if (r < end) a.part_ml[at] = make_float2(ref, sum);
             }
-            if (real && !it.last) a.part_ml[part_at] = make_float2(dead ? 0.0f : ref, sum);
             __syncwarp();
             tmem_before_sync();
             mbar_arrive(&sh->o_empty[h]);
+        }
+        if (dead) {  // a wait has run out: rows that are not done say so
+            const float nan = __int_as_float(0x7fffffff);
+            for (int64_t w = done_work < 0 ? blockIdx.x : done_work + gridDim.x; w < total; w += gridDim.x) {
+                TileItem it;
+                if (!tile_item(a, prefix, tiles_per_segment, w, it)) continue;
+                const int r = it.row0 + h * kHalf + row;
+                if (r >= it.row0 + it.rows) continue;
+                int qrow, head;
+                tile_row(a, it.kvh, r, qrow, head);
+                T* const out = static_cast<T*>(a.out) + (it.seg.q0 + qrow) * a.o_row + head * a.o_head;
+                const int64_t at = ((int64_t)it.split * a.q_total + it.seg.q0 + qrow) * a.heads + head;
+                if (!it.last) a.part_ml[at] = make_float2(0.0f, nan);
+                for (int d = 0; it.last && d < a.dim; d += 2) *reinterpret_cast<uint32_t*>(out + d) = pack2<T>(nan, nan);
+            }
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
@@ -439,88 +533,128 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                 const int ksteps = (a.dim + 15) >> 4;
                 const uint32_t idesc_pv = instr_desc<T>(16 * ksteps, true), idesc_qk = instr_desc<T>(0, false);
                 uint32_t slot = 0, tile = 0, items = 0;
-                uint32_t half_tiles[2] = {0, 0}, half_items[2] = {0, 0};
+                uint32_t turns[2] = {0, 0}, weights[2] = {0, 0}, half_items[2] = {0, 0};  // scores issued, weights used
                 bool ok = true;
                 auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, tile_wait(bar, parity, a.status)); };
                 auto commit = [&](uint64_t* bar) {
                     if (elect_one()) mma_commit(bar);
                     __syncwarp();
                 };
-                auto meta_at = [&](uint32_t n) { return __shfl_sync(0xffffffffu, sh->meta[n & 15], 0); };
                 auto full_wait = [&](uint32_t n) { wait(&sh->full[n % Shape::kStages], (n / Shape::kStages) & 1); };
                 auto slot_at = [&](uint32_t n) { return ring + (n % Shape::kStages) * Shape::kStageBytes; };
-                auto scores = [&](int h, uint32_t k_slot, int meta) {  // S_h = Q_h K^T over the visible keys
-                    const int n = max(16, ((meta & 0xffff) + 15) & ~15);
-                    const uint32_t idesc = idesc_qk + ((uint32_t)(n >> 3) << 17);
-                    const uint32_t qa = desc_low(q_base + h * Shape::kStageBytes, 0), ka = desc_low(slot_at(k_slot), 0);
+                // S_h = Q_h K^T over keys [64 sub, 64 sub + keys) of the tile in k_slot
+                auto scores = [&](int h, uint32_t k_slot, int sub, int keys, int flags) {
+                    const int n = max(16, (keys + 15) & ~15);
+                    const uint32_t idesc = idesc_qk + ((uint32_t)(n >> 3) << 17), d = tmem + 128u * h + 64u * (turns[h] & 1);
+                    const uint32_t qa = desc_low(q_base + h * Shape::kStageBytes, 0), ka = desc_low(slot_at(k_slot) + 8192u * sub, 0);
                     if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < 4 * DB; ++k) {
                             const uint32_t off = ((uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32u) >> 4;
-                            if (k < ksteps) mma_ss(tmem + 128u * h, desc_of(qa + off), desc_of(ka + off), idesc, k > 0);
+                            if (k < ksteps) mma_ss(d, desc_of(qa + off), desc_of(ka + off), idesc, k > 0);
                         }
-                        sh->half_meta[h][half_tiles[h] & 3] = meta;
-                        mma_commit(&sh->s_full[h]);
-                        mbar_arrive(&sh->s_full[h]);
+                        sh->half_meta[h][turns[h] & 3] = keys | flags;
+                        mma_commit(&sh->s_full[h][turns[h] & 1]);
+                        mbar_arrive(&sh->s_full[h][turns[h] & 1]);
                     }
                     __syncwarp();
+                    ++turns[h];
                 };
-                for (int64_t w = blockIdx.x; w < total && ok; w += gridDim.x) {
-                    TileItem it;
-                    if (!tile_item(a, prefix, tiles_per_segment, w, it)) continue;
-                    const int halves = it.rows > kHalf ? 2 : 1;
+                for (;;) {
                     wait(&sh->q_full, items & 1);
-                    full_wait(slot);
+                    if (!ok) break;
+                    const int rows = __shfl_sync(0xffffffffu, sh->info[items & 3].rows, 0);
+                    if (rows == 0) break;  // no more items
+                    const int halves = rows > kHalf ? 2 : 1, tag = (int)(items & 3) << kItemShift;
+                    // One walk over the turns of the item: the scores of turn j + 1 are issued ahead of the products
+                    // of turn j.  (k_slot, k_sub, k_keys): where the scores are; v_*: where the products are.
+                    uint32_t k_slot = slot;
+                    full_wait(k_slot);
                     if (!ok) break;
                     tmem_after_sync();
-                    int meta = meta_at(tile);
-                    for (int h = 0; h < halves; ++h) scores(h, slot, meta);
-                    commit(&sh->empty[slot % Shape::kStages]);
-                    if (meta >> 16) commit(&sh->q_empty);
-                    ++slot;
-                    for (bool first = true;; first = false) {
-                        const bool last = meta >> 16;
-                        const int steps = max(1, ((meta & 0xffff) + 15) >> 4);
-                        int next = 0;
-                        full_wait(slot);
-                        for (int h = 0; h < halves; ++h) {
-                            wait(&sh->p_full[h], half_tiles[h] & 1);
-                            if (first) wait(&sh->o_empty[h], (half_items[h] & 1) ^ 1);
-                            if (!ok) break;
-                            tmem_after_sync();
-                            ++half_tiles[h];
-                            const uint32_t va = desc_low(slot_at(slot), kBlockBytes);
-                            if (elect_one()) {
-#pragma unroll
-                                for (int k = 0; k < 8; ++k)
-                                    if (k < steps)
-                                        mma_ts(tmem + 256u + 128u * h, tmem + 128u * h + 8u * k, desc_of(va + 128u * k), idesc_pv,
-                                               !first || k > 0);
-                                if (last) mma_commit(&sh->o_full[h]);
+                    int k_meta = __shfl_sync(0xffffffffu, sh->meta[tile & 15], 0), k_sub = 0;
+                    ++tile;
+                    bool more = true, first = true;
+                    int v_keys = 0, v_sub = 0;
+                    uint32_t v_slot = 0;
+                    bool v_frees = false;
+                    for (;;) {
+                        int keys = 0, sub = 0;
+                        uint32_t at = 0;
+                        bool frees = false;
+                        if (more) {
+                            const int left = (k_meta & 0xffff) - kSub * k_sub;
+                            keys = min(left, kSub);
+                            sub = k_sub;
+                            at = k_slot;
+                            frees = left <= kSub;  // the tile's last turn
+                            const bool last = frees && (k_meta >> 16);
+                            for (int h = 0; h < halves; ++h) scores(h, k_slot, sub, keys, (last ? kLast : 0) | tag);
+                            if (frees) {
+                                commit(&sh->empty[k_slot % Shape::kStages]);
+                                if (last) commit(&sh->q_empty);
                             }
-                            __syncwarp();
-                            if (last) {
-                                ++half_items[h];
-                            } else {
-                                if (h == 0) {
-                                    full_wait(slot + 1);
-                                    if (!ok) break;
-                                    next = meta_at(tile + 1);
+                            more = !last;
+                            ++k_sub;
+                        }
+                        if (!first) {
+                            // O_h += P_h V over the turn before
+                            if (v_sub == 0) full_wait(v_slot);
+                            const bool start = v_slot == slot + 1 && v_sub == 0, stop = keys == 0 && !frees;
+                            const uint32_t va = desc_low(slot_at(v_slot) + 8192u * v_sub, kBlockBytes);
+                            const int steps = max(1, (v_keys + 15) >> 4);
+                            for (int h = 0; h < halves && ok; ++h) {
+                                wait(&sh->p_full[h][weights[h] & 1], (weights[h] >> 1) & 1);
+                                if (start) wait(&sh->o_empty[h], (half_items[h] & 1) ^ 1);
+                                if (!ok) break;
+                                tmem_after_sync();
+                                const uint32_t pa = tmem + 128u * h + 64u * (weights[h] & 1);
+                                if (elect_one()) {
+#pragma unroll
+                                    for (int k = 0; k < 4; ++k)
+                                        if (k < steps)
+                                            mma_ts(tmem + 256u + 128u * h, pa + 8u * k, desc_of(va + 128u * k), idesc_pv, !start || k > 0);
+                                    mma_commit(&sh->pv_done[h]);
                                 }
-                                scores(h, slot + 1, next);
+                                __syncwarp();
+                                ++weights[h];
+                                if (stop) ++half_items[h];
+                            }
+                            if (!ok) break;
+                            if (v_frees) commit(&sh->empty[v_slot % Shape::kStages]);
+                            if (stop) {
+                                slot = v_slot + 1;
+                                break;
                             }
                         }
-                        if (!ok) break;
-                        commit(&sh->empty[slot % Shape::kStages]);
-                        ++slot;
-                        ++tile;
-                        if (last) break;
-                        commit(&sh->empty[slot % Shape::kStages]);
-                        if (next >> 16) commit(&sh->q_empty);
-                        ++slot;
-                        meta = next;
+                        first = false;
+                        v_keys = keys;
+                        v_sub = sub;
+                        v_slot = at + 1;
+                        v_frees = frees;
+                        if (more && frees) {  // on to the next tile's keys
+                            k_slot += 2;
+                            k_sub = 0;
+                            full_wait(k_slot);
+                            if (!ok) break;
+                            tmem_after_sync();
+                            k_meta = __shfl_sync(0xffffffffu, sh->meta[tile & 15], 0);
+                            ++tile;
+                        }
                     }
+                    if (!ok) break;
                     ++items;
+                }
+                if (ok) {  // the softmax groups may leave
+                    if (elect_one()) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            sh->half_meta[h][turns[h] & 3] = kStop;
+                            mbar_arrive(&sh->s_full[h][turns[h] & 1]);
+                            mbar_arrive(&sh->s_full[h][turns[h] & 1]);
+                        }
+                    }
+                    __syncwarp();
                 }
                 commit(&sh->done);  // nothing of this CTA is under way when it gives its memory back
                 tile_wait(&sh->done, 0, a.status);
@@ -538,16 +672,36 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
             for (int64_t w = blockIdx.x; w < total && !ld.dead; w += gridDim.x) {
                 TileItem it;
                 if (!tile_item(a, prefix, tiles_per_segment, w, it)) continue;
-                ld.wait(&sh->q_empty, (items & 1) ^ 1);
-                if (ld.dead) break;
-                const T* const q = static_cast<const T*>(a.q) + it.seg.q0 * a.q_row + (int64_t)it.kvh * a.group * a.q_head;
-                ld.rows(q_base, it.rows > kHalf ? 2 * kHalf : kHalf, [&](int r) -> const char* {
-                    if (r >= it.rows) return nullptr;
-                    const int vr = it.row0 + r, qrow = vr / a.group;
-                    return reinterpret_cast<const char*>(q + qrow * a.q_row + (vr - qrow * a.group) * a.q_head);
-                });
-                ld.issued(&sh->q_full);
-                ++items;
+                // the queries follow the first keys and values: their place is free only when the last item's scores are made
+                auto load_queries = [&]() {
+                    ld.wait(&sh->q_empty, (items & 1) ^ 1);
+                    if (ld.dead) return;
+                    const int64_t row = 2 * a.q_row, head = 2 * a.q_head;
+                    const char* const q = static_cast<const char*>(a.q) + it.seg.q0 * row + (int64_t)it.kvh * a.group * head;
+                    for (int b = 0; b < it.rows; b += kHalf) {
+                        if (a.group == 1 && it.rows - b >= kHalf)
+                            ld.full_rows(q_base + (b / kHalf) * Shape::kStageBytes, q + (it.row0 + b) * row, row);
+                        else
+                            ld.rows(q_base + (b / kHalf) * Shape::kStageBytes, kHalf, [&](int r) -> const char* {
+                                int qrow, hd;
+                                tile_row(a, 0, it.row0 + b + r, qrow, hd);
+                                return b + r < it.rows ? q + qrow * row + hd * head : nullptr;
+                            });
+                    }
+                    if (warp == 9 && lane == 0) {
+                        TileInfo& info = sh->info[items & 3];
+                        info.q0 = it.seg.q0;
+                        info.work = w;
+                        info.kvh = it.kvh;
+                        info.split = it.split;
+                        info.row0 = it.row0;
+                        info.rows = it.rows;
+                        info.last = it.last;
+                    }
+                    ld.issued(&sh->q_full);
+                    ++items;
+                };
+                bool queries = false;
                 const char* const k = reinterpret_cast<const char*>(static_cast<const T*>(a.k) + it.seg.k0 * a.k_row + it.kvh * a.k_head);
                 const char* const v = reinterpret_cast<const char*>(static_cast<const T*>(a.v) + it.seg.k0 * a.v_row + it.kvh * a.v_head);
                 const uint8_t* const mask = a.mask ? a.mask + it.seg.k0 : nullptr;
@@ -599,6 +753,10 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                         ld.issued(&sh->full[n % Shape::kStages]);
                         ++ld.slot;
                     }
+                    if (!queries && !ld.dead) {
+                        load_queries();
+                        queries = true;
+                    }
                     if (mask) {  // what is left over moves to the front
                         listed -= take;
                         int rest[4];
@@ -613,7 +771,13 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                     }
                 }
             }
+            if (!ld.dead) ld.wait(&sh->q_empty, (items & 1) ^ 1);
             ld.flush();
+            if (!ld.dead) {  // an item without rows: there are no more
+                if (warp == 9 && lane == 0) sh->info[items & 3].rows = 0;
+                __syncwarp();
+                mbar_arrive(&sh->q_full);
+            }
         }
     }
     tmem_before_sync();
