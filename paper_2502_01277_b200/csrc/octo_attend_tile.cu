@@ -47,7 +47,7 @@ struct TileInfo {
 struct TileShared {
     uint64_t full[8], empty[8];
     uint64_t q_full, q_empty, done;
-    uint64_t s_full[2][2], p_full[2][2], pv_done[2], o_empty[2];
+    uint64_t s_full[2][2], p_full[2][2], pv_done[2][2], o_empty[2];  // [half][turn & 1]: see below
     int meta[16];         // per key tile, by the loaders: visible keys | last << 16
     int half_meta[2][4];  // per half and turn, by the issuing warp: keys | kLast | item << kItemShift | kStop
     TileInfo info[4];
@@ -55,6 +55,9 @@ struct TileShared {
     int list[3][kListInts];
     uint4 stage[8][32 * 4];  // per softmax warp: 32 rows of 32 elements on their way out
 };
+// A wait names the parity of one phase, so a barrier may be at most one phase away from the one that is waited for.  The
+// scores, weights and products of a half therefore have a barrier for even and one for odd turns: turn n + 2 is not
+// begun before turn n's weights are there, but turn n + 1 may be through before anyone has asked for turn n.
 constexpr int kLast = 1 << 8, kStop = 1 << 9, kItemShift = 16;
 
 // ---- tensor core and tensor memory ----------------------------------------------------------------------
@@ -288,7 +291,8 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
             mbar_init(&sh->s_full[h][1], 2);
             mbar_init(&sh->p_full[h][0], kHalf);
             mbar_init(&sh->p_full[h][1], kHalf);
-            mbar_init(&sh->pv_done[h], 1);
+            mbar_init(&sh->pv_done[h][0], 1);
+            mbar_init(&sh->pv_done[h][1], 1);
             mbar_init(&sh->o_empty[h], kHalf);
         }
         mbar_fence_init();
@@ -374,7 +378,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                         sum *= f;
                         ref = now;
                         if (!first) {  // (of the products, all but the last turn's are complete: the scores came after them)
-                            if (!__all_sync(0xffffffffu, tile_wait(&sh->pv_done[h], (turn - 1) & 1, a.status))) dead = true;
+                            if (!__all_sync(0xffffffffu, tile_wait(&sh->pv_done[h][(turn - 1) & 1], ((turn - 1) >> 1) & 1, a.status))) dead = true;
                             tmem_after_sync();
                             for (int c = 0; c < o_chunks; ++c) {
                                 uint32_t o[32];
@@ -404,6 +408,12 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                             }
                             tmem_landed(s[1]);
                         }
+                        if (take < 32 * (c + 1)) {  // columns behind the last visible key weigh nothing
+                            const uint32_t none = __float_as_uint(sc < 0.0f ? INFINITY : -INFINITY);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (32 * c + i >= take) s[c][i] = none;
+                        }
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const uint32_t* const in = s[c] + 2 * i;
@@ -411,10 +421,6 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                             asm("mov.b64 {%0, %1}, %2;"
                                 : "=f"(x), "=f"(y)
                                 : "l"(fma_f32x2(f32x2(__uint_as_float(in[0]), __uint_as_float(in[1])), sc2, minus2)));
-                            if (take < kSub) {  // columns behind the last visible key
-                                if (32 * c + 2 * i >= take) x = -INFINITY;
-                                if (32 * c + 2 * i + 1 >= take) y = -INFINITY;
-                            }
                             top = max3(top, x, y);
                             x = ex2(x);
                             y = ex2(y);
@@ -442,9 +448,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
             if (dead || (meta & kStop)) break;
             // the half's rows of the result
             const TileInfo it = sh->info[meta >> kItemShift];
-            // the products of the last turn; those of the turn before may still be under way, and their phase comes first
-            if (!__all_sync(0xffffffffu, tile_wait(&sh->pv_done[h], turn & 1, a.status) &&
-                                             tile_wait(&sh->pv_done[h], (turn - 1) & 1, a.status))) {
+            if (!__all_sync(0xffffffffu, tile_wait(&sh->pv_done[h][(turn - 1) & 1], ((turn - 1) >> 1) & 1, a.status))) {
                 dead = true;
                 break;
             }
@@ -614,7 +618,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                                     for (int k = 0; k < 4; ++k)
                                         if (k < steps)
                                             mma_ts(tmem + 256u + 128u * h, pa + 8u * k, desc_of(va + 128u * k), idesc_pv, !start || k > 0);
-                                    mma_commit(&sh->pv_done[h]);
+                                    mma_commit(&sh->pv_done[h][weights[h] & 1]);
                                 }
                                 __syncwarp();
                                 ++weights[h];
