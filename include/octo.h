@@ -555,7 +555,7 @@ typedef struct {
     int32_t head_dim;                 /* a multiple of 8, 8 .. 128                                         */
     int64_t q_total, k_total;         /* rows of q and out; rows of k, v and the mask: at most 2^30, and   */
                                       /* q_total * heads < 2^31                                            */
-    octo_heads_t q, k, v, out;        /* 16-byte aligned, strides multiples of 8 elements                  */
+    octo_heads_t q, k, v, out;        /* 16-byte aligned; strides multiples of 8 elements, 0 .. 2^30 - 8    */
     const int32_t* d_q_offsets;       /* [segments + 1] non-decreasing, or NULL                            */
     const int32_t* d_k_offsets;       /* [segments + 1] non-decreasing, or NULL                            */
     int64_t q_rows, k_rows;           /* rows per step of the offsets, >= 1                                */

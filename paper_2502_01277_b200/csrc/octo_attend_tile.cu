@@ -5,8 +5,10 @@
 //   warps 0-3, 4-7   one softmax group per half (128 rows, a thread per row): scores from tensor memory, running
 //                    maximum and sum in registers, weights back into tensor memory over the scores they came from;
 //                    at the end the half's rows of the result.
-//   warp 8           issues all matrix instructions: S_h = Q_h K^T, O_h += P_h V.
-//   warps 9-11       fetch queries, keys and values with 16-byte asynchronous copies into shared memory, in the
+//   warps 8, 9       issue the matrix instructions of one half each: S_h = Q_h K^T, O_h += P_h V.  (One warp for both was
+//                    what the kernel waited for: its waits, about 150 clocks each though satisfied, left the tensor
+//                    cores idle for 40 % of the time.)
+//   warps 10, 11     fetch queries, keys and values with 16-byte asynchronous copies into shared memory, in the
 //                    128-byte swizzle that the matrix instructions read.  Copies by row (rather than by tensor
 //                    map) let a tile consist of the VISIBLE keys only, wherever they lie: hidden keys cost a byte
 //                    of mask and nothing else, and what they hold is never looked at.
@@ -26,10 +28,12 @@ namespace octo {
 constexpr int kTileThreads = 384;
 constexpr int kHalf = 128;            // rows of a half, keys of a tile
 constexpr int kSub = 64;              // keys of a turn
-constexpr int kLoaders = 96;
+constexpr int kLoadWarps = 2, kLoaders = 32 * kLoadWarps;
 constexpr int kBlockBytes = 128 * 128;  // 128 rows of 64 elements
 constexpr int kListInts = 256;
-constexpr float kSlack = 8.0f;        // growth of the maximum, as a power of two, before the reference follows
+constexpr float kSlack = 8.0f;        // growth of the maximum, as a power of two, before the reference has to follow
+constexpr float kMostInTurn = 1024.0f;  // sum of a turn's 64 weights up to which it does not
+constexpr float kGrown = 4.0f;          // (64 weights that sum to more than 1024: one is above 2^4)
 
 template <int DB>
 struct TileShape {
@@ -46,13 +50,13 @@ struct TileInfo {
 
 struct TileShared {
     uint64_t full[8], empty[8];
-    uint64_t q_full, q_empty, done;
+    uint64_t q_full, q_empty, done[2];
     uint64_t s_full[2][2], p_full[2][2], pv_done[2][2], o_empty[2];  // [half][turn & 1]: see below
     int meta[16];         // per key tile, by the loaders: visible keys | last << 16
     int half_meta[2][4];  // per half and turn, by the issuing warp: keys | kLast | item << kItemShift | kStop
     TileInfo info[4];
     uint32_t tmem;
-    int list[3][kListInts];
+    int list[kLoadWarps][kListInts];
     uint4 stage[8][32 * 4];  // per softmax warp: 32 rows of 32 elements on their way out
 };
 // A wait names the parity of one phase, so a barrier may be at most one phase away from the one that is waited for.  The
@@ -127,6 +131,56 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ void halves_of(unsigned long long v, float& x, float& y) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
+}
+__device__ __forceinline__ unsigned long long pair_of(float v) { return f32x2(v, v); }
+
+// 2^x and 2^y on the multiply-add pipe, for x, y <= kSlack: x = n + f with n whole and |f| <= 1/2, a polynomial for 2^f (degree
+// 4, fitted to the least relative error on [-1/2, 1/2], 2.7e-6) and n added to its exponent.  Arguments below
+// -126 count as -126 (a weight that no sum keeps); NaN gives a number above 2^126 or NaN.
+__device__ __forceinline__ void ex2_by_polynomial(float& x, float& y) {
+    const unsigned long long magic = pair_of(12582912.0f);  // 1.5 * 2^23: adding it rounds to whole numbers
+    const unsigned long long v = f32x2(max_nan(x, -126.0f), max_nan(y, -126.0f));
+    const unsigned long long n = add_f32x2(v, magic);
+    const unsigned long long f = fma_f32x2(add_f32x2(n, pair_of(-12582912.0f)), pair_of(-1.0f), v);
+    unsigned long long q = fma_f32x2(f, pair_of(0x1.3997d4p-7f), pair_of(0x1.ca1440p-5f));
+    q = fma_f32x2(q, f, pair_of(0x1.ec06dap-3f));
+    q = fma_f32x2(q, f, pair_of(0x1.62e0dcp-1f));
+    q = fma_f32x2(q, f, pair_of(0x1.ffffe8p-1f));
+    float nx, ny;
+    halves_of(n, nx, ny);
+    halves_of(q, x, y);
+    x = __uint_as_float(__float_as_uint(x) + (__float_as_uint(nx) << 23));
+    y = __uint_as_float(__float_as_uint(y) + (__float_as_uint(ny) << 23));
+}
+
+// Weights of 32 scores: 2^(s * scale + minus), packed in the type of the values, and their sum (of the unrounded ones).
+// The special-function unit takes eight clocks for a warp's exponentials, and both halves' warps share it: without EXACT
+// every fourth pair goes to the multiply-add pipe instead.  `top`: the largest exponent among those.
+template <typename T, bool EXACT>
+__device__ __forceinline__ void weigh(const uint32_t* s, unsigned long long scale, unsigned long long minus, uint32_t* p,
+                                      unsigned long long& sum, float& top) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float x, y;
+        halves_of(fma_f32x2(f32x2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale, minus), x, y);
+        if (!EXACT && false) {
+            top = max3(top, x, y);
+            ex2_by_polynomial(x, y);
+        } else {
+            x = ex2(x);
+            y = ex2(y);
+        }
+        sum = add_f32x2(sum, f32x2(x, y));
+        p[i] = pack2<T>(x, y);  // what the matrix instruction takes
+    }
 }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool take) {
@@ -223,45 +277,62 @@ struct Loader {
         if (!__all_sync(0xffffffffu, tile_wait(bar, parity, status))) dead = true;
     }
 
-    // A warp takes every third group of 8 rows, kRowsAtOnce rows per instruction; the swizzle of a lane's row inside
+    // The warps take groups of 8 rows in turn, kRowsAtOnce rows per instruction; the swizzle of a lane's row inside
     // its group, and so its place in shared memory, is the same for every group.
     static constexpr int kLanesPerRow = 8 * DB, kRowsAtOnce = 32 / kLanesPerRow, kTurns = 8 / kRowsAtOnce;
+    static constexpr int kGroups = 16 / kLoadWarps, kOwn = kGroups * kTurns;  // groups of a warp, rows of a lane
     uint32_t place[kTurns];  // of the lane's piece of row kRowsAtOnce * i + its own in a group
     bool wide;               // the lane's piece lies inside the head
+    __device__ __forceinline__ int own() const { return lane / kLanesPerRow; }
+    __device__ __forceinline__ int column() const { return lane & (kLanesPerRow - 1); }
     __device__ __forceinline__ void layout(int dim_bytes) {
-        const int c = lane & (kLanesPerRow - 1), own = lane / kLanesPerRow;
-        wide = c * 16 < dim_bytes;
+        wide = column() * 16 < dim_bytes;
 #pragma unroll
         for (int i = 0; i < kTurns; ++i) {
-            const int r = kRowsAtOnce * i + own;
-            place[i] = (uint32_t)(c >> 3) * kBlockBytes + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ r) << 4);
+            const int r = kRowsAtOnce * i + own();
+            place[i] = (uint32_t)(column() >> 3) * kBlockBytes + (uint32_t)r * 128u + (uint32_t)(((column() & 7) ^ r) << 4);
         }
     }
-    // Rows [0, count) of a tile, count a multiple of 8; row_at(r) gives a row's address or null for zeros.
+    // The lane's rows of a tile of 128: row(j) for j < kOwn.
+    __device__ __forceinline__ int row(int j) const { return 8 * (warp + kLoadWarps * (j / kTurns)) + kRowsAtOnce * (j % kTurns) + own(); }
+    // One tile: key(r) is the row of `src` that row r of the tile holds, r < take; zeros from there on.
     template <typename F>
-    __device__ __forceinline__ void rows(uint32_t dst, int count, F row_at) {
-        const int c = lane & (kLanesPerRow - 1), own = lane / kLanesPerRow;
-        for (int g = warp; g < (count >> 3); g += 3) {
-            const uint32_t at = dst + (uint32_t)g * 1024u;
+    __device__ __forceinline__ void tile(uint32_t dst, int take, const char* src, int stride, F key) {
+        src += column() * 16;
+        const int groups = (max(16, (take + 15) & ~15)) >> 3;  // that the matrix instructions read
+#pragma unroll 1
+        for (int b = 0; b < kOwn; b += 8) {
+            if (warp + kLoadWarps * (b / kTurns) >= groups) break;
 #pragma unroll
-            for (int i = 0; i < kTurns; ++i) {
-                const char* p = row_at(8 * g + kRowsAtOnce * i + own);
-                const bool take = wide && p != nullptr;
-                cp_async16(at + place[i], take ? p + c * 16 : zero_row, take);
+            for (int i = 0; i < 8; ++i) {
+                const int g = warp + kLoadWarps * ((b + i) / kTurns), r = row(b + i);
+                const bool take_it = wide && r < take;
+                const char* const p = take_it ? src + (int64_t)key(r) * stride : zero_row;
+                if (g < groups) cp_async16(dst + (uint32_t)g * 1024u + place[i % kTurns], p, take_it);
             }
         }
     }
-    // 128 rows that lie side by side from `src` on, `stride` bytes apart.
-    __device__ __forceinline__ void full_rows(uint32_t dst, const char* src, int64_t stride) {
-        const int c = lane & (kLanesPerRow - 1), own = lane / kLanesPerRow;
-        const char* p = wide ? src + (8 * warp + own) * stride + c * 16 : zero_row;
-        const int64_t turn = wide ? kRowsAtOnce * stride : 0, group = wide ? 24 * stride : 0;
+    // 128 rows that lie side by side from `src` on.
+    __device__ __forceinline__ void full_tile(uint32_t dst, const char* src, int stride) {
+        const char* p = wide ? src + (int64_t)(8 * warp + own()) * stride + column() * 16 : zero_row;
+        const int64_t turn = wide ? kRowsAtOnce * stride : 0, group = wide ? (int64_t)(8 * kLoadWarps) * stride : 0;
         uint32_t at = dst + (uint32_t)warp * 1024u;
-        for (int g = warp; g < 16; g += 3) {
+#pragma unroll 4
+        for (int g = 0; g < kGroups; ++g) {
 #pragma unroll
             for (int i = 0; i < kTurns; ++i) cp_async16(at + place[i], p + i * turn, wide);
             p += group;
-            at += 3 * 1024u;
+            at += kLoadWarps * 1024u;
+        }
+    }
+    // The queries' tile; at(r) gives a row's address, or null for zeros.
+    template <typename F>
+    __device__ __forceinline__ void queries(uint32_t dst, F at) {
+#pragma unroll 8
+        for (int j = 0; j < kOwn; ++j) {
+            const char* p = at(row(j));
+            const bool take = wide && p != nullptr;
+            cp_async16(dst + (uint32_t)(warp + kLoadWarps * (j / kTurns)) * 1024u + place[j % kTurns], take ? p + column() * 16 : zero_row, take);
         }
     }
     const char* zero_row;  // any valid address
@@ -281,11 +352,12 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
     if (threadIdx.x == 0) {
         for (int i = 0; i < Shape::kStages; ++i) {
             mbar_init(&sh->full[i], kLoaders);
-            mbar_init(&sh->empty[i], 1);
+            mbar_init(&sh->empty[i], 2);
         }
         mbar_init(&sh->q_full, kLoaders);
-        mbar_init(&sh->q_empty, 1);
-        mbar_init(&sh->done, 1);
+        mbar_init(&sh->q_empty, 2);
+        mbar_init(&sh->done[0], 1);
+        mbar_init(&sh->done[1], 1);
         for (int h = 0; h < 2; ++h) {
             mbar_init(&sh->s_full[h][0], 2);
             mbar_init(&sh->s_full[h][1], 2);
@@ -339,40 +411,77 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
         const float sc = a.scale_log2;
         const int o_chunks = (a.dim + 31) >> 5;
         uint32_t turn = 0;  // turns so far; the scores of turn n are in buffer n & 1
+        const unsigned long long sc2 = pair_of(sc);
+        auto scores_at = [&](uint32_t n) { return lanes + 128u * h + 64u * (n & 1); };
         int64_t done_work = -1;
         bool dead = false;
         for (;;) {
             float ref = -INFINITY, sum = 0.0f;  // what the exponents are taken against; sum of the weights
-            bool first = true;
+            bool look = true;    // the scores have to be looked through before they are weighed
+            bool first = true, ahead = false;  // ahead: the turn's scores are on their way into s0 already
             int meta = 0;
+            uint32_t s0[32], s1[32], p[32];
             while (!(meta & (kLast | kStop))) {
-                if (!__all_sync(0xffffffffu, tile_wait(&sh->s_full[h][turn & 1], (turn >> 1) & 1, a.status))) {
-                    dead = true;
-                    break;
+                if (!ahead) {
+                    if (!__all_sync(0xffffffffu, tile_wait(&sh->s_full[h][turn & 1], (turn >> 1) & 1, a.status))) {
+                        dead = true;
+                        break;
+                    }
+                    tmem_after_sync();
                 }
-                tmem_after_sync();
                 meta = sh->half_meta[h][turn & 3];
                 if (meta & kStop) break;
                 const int take = meta & 0xff;
-                const uint32_t s_at = lanes + 128u * h + 64u * (turn & 1);
-                // Weights against the reference so far, and the scores' maximum beside them: the exponentials do not wait
-                // for the maximum.  Only if a row's has outgrown the reference (and for the first turn, whose
-                // scores are looked through before) is the reference moved and the turn, still in tensor memory, taken again.
-                uint32_t p[32];
+                const uint32_t s_at = scores_at(turn);
+                if (!ahead) tmem_ld32(s_at, s0);
+                tmem_landed(s0);
+                ahead = false;
                 unsigned long long part = 0ull;
-                for (bool look = first;;) {
-                    if (look) {
-                        float top = -INFINITY;
+                bool again = look || take < kSub;
+                if (!again) {
+                    // Weights against the reference so far: the exponentials do not wait for a maximum.
+                    const unsigned long long minus = pair_of(-ref);
+                    float top = -INFINITY;
+                    tmem_ld32(s_at + 32, s1);
+                    weigh<T, false>(s0, sc2, minus, p, part, top);
+                    tmem_landed(s1);
+                    // the next turn's scores are fetched beside this one's second half, if they are there
+                    if (!(meta & kLast) && __all_sync(0xffffffffu, mbar_test_wait(&sh->s_full[h][(turn + 1) & 1], ((turn + 1) >> 1) & 1))) {
+                        tmem_after_sync();
+                        tmem_ld32(scores_at(turn + 1), s0);
+                        ahead = true;
+                    }
+                    weigh<T, false>(s1, sc2, minus, p + 16, part, top);
+                    float x, y;
+                    halves_of(part, x, y);
+                    // A weight far above the reference shows in the sum (false for NaN: it comes through the weights).
+                    again = __any_sync(0xffffffffu, x + y > kMostInTurn || top > kSlack);
+                }
+                if (again) {
+                    // The first turn, the last one where it is not full, and turns in which a row has outgrown its reference: the
+                    // scores, still in tensor memory, are looked through, the reference follows, and they are weighed exactly.
+                    if (ahead) tmem_landed(s0);  // (taken once more below)
+                    ahead = false;
+                    const uint32_t none = __float_as_uint(sc < 0.0f ? INFINITY : -INFINITY);  // behind the last visible key
+                    float top = -INFINITY;
+                    tmem_ld32(s_at, s0);
+                    tmem_landed(s0);
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            if (32 * c >= take) break;
-                            uint32_t s[32];
-                            tmem_ld32(s_at + 32 * c, s);
-                            tmem_landed(s);
+                    for (int i = 0; i < 32; ++i) {
+                        if (i >= take) s0[i] = none;
+                        else top = fmaxf(top, __uint_as_float(s0[i]) * sc);
+                    }
+                    if (take > 32) {
+                        tmem_ld32(s_at + 32, s1);
+                        tmem_landed(s1);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (32 * c + i < take) top = fmaxf(top, __uint_as_float(s[i]) * sc);
+                        for (int i = 0; i < 32; ++i) {
+                            if (32 + i >= take) s1[i] = none;
+                            else top = fmaxf(top, __uint_as_float(s1[i]) * sc);
                         }
+                    }
+                    const bool grown = top > ref + kGrown || (ref == -INFINITY && top > -INFINITY);
+                    if (__any_sync(0xffffffffu, grown)) {
                         const float now = fmaxf(ref, top);
                         const float f = now == -INFINITY ? 1.0f : ex2(ref - now);
                         sum *= f;
@@ -381,65 +490,30 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                             if (!__all_sync(0xffffffffu, tile_wait(&sh->pv_done[h][(turn - 1) & 1], ((turn - 1) >> 1) & 1, a.status))) dead = true;
                             tmem_after_sync();
                             for (int c = 0; c < o_chunks; ++c) {
-                                uint32_t o[32];
-                                tmem_ld32(o_at + 32 * c, o);
-                                tmem_landed(o);
+                                tmem_ld32(o_at + 32 * c, p);
+                                tmem_landed(p);
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                                tmem_st32(o_at + 32 * c, o);
+                                for (int i = 0; i < 32; ++i) p[i] = __float_as_uint(__uint_as_float(p[i]) * f);
+                                tmem_st32(o_at + 32 * c, p);
                             }
                         }
                     }
-                    const float minus = ref == -INFINITY ? 0.0f : -ref;
-                    const unsigned long long sc2 = f32x2(sc, sc), minus2 = f32x2(minus, minus);
-                    float top = -INFINITY;  // above the reference
+                    look = __any_sync(0xffffffffu, ref == -INFINITY);
+                    const unsigned long long minus = pair_of(ref == -INFINITY ? 0.0f : -ref);
                     part = 0ull;
-                    uint32_t s[2][32];
-                    tmem_ld32(s_at, s[0]);
-                    tmem_landed(s[0]);
-                    if (take > 32) tmem_ld32(s_at + 32, s[1]);
+                    weigh<T, true>(s0, sc2, minus, p, part, top);
+                    if (take > 32) {
+                        weigh<T, true>(s1, sc2, minus, p + 16, part, top);
+                    } else {  // (the matrix instruction reads the first 32 weights then)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        if (c > 0) {
-                            if (take <= 32) {  // (the matrix instruction reads the first 32 weights then)
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) p[16 + i] = 0u;
-                                break;
-                            }
-                            tmem_landed(s[1]);
-                        }
-                        if (take < 32 * (c + 1)) {  // columns behind the last visible key weigh nothing
-                            const uint32_t none = __float_as_uint(sc < 0.0f ? INFINITY : -INFINITY);
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (32 * c + i >= take) s[c][i] = none;
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const uint32_t* const in = s[c] + 2 * i;
-                            float x, y;
-                            asm("mov.b64 {%0, %1}, %2;"
-                                : "=f"(x), "=f"(y)
-                                : "l"(fma_f32x2(f32x2(__uint_as_float(in[0]), __uint_as_float(in[1])), sc2, minus2)));
-                            top = max3(top, x, y);
-                            x = ex2(x);
-                            y = ex2(y);
-                            part = add_f32x2(part, f32x2(x, y));
-                            // the weights in the type of the values: what the matrix instruction takes (the sum keeps them unrounded)
-                            p[16 * c + i] = pack2<T>(x, y);
-                        }
+                        for (int i = 16; i < 32; ++i) p[i] = 0u;
                     }
-                    // (false for NaN: it leaves the reference and comes through the exponentials)
-                    if (look || !__any_sync(0xffffffffu, (ref == -INFINITY && top > -INFINITY) || top > kSlack)) break;
-                    look = true;
                 }
                 first = false;
                 tmem_st32(s_at, p);
-                {
-                    float x, y;
-                    asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(part));
-                    sum += x + y;
-                }
+                float x, y;
+                halves_of(part, x, y);
+                sum += x + y;
                 tmem_wait_st();
                 tmem_before_sync();
                 mbar_arrive(&sh->p_full[h][turn & 1]);
@@ -529,148 +603,145 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-        if (warp == 8) {
-            {
-                // ---------------- matrix instructions ----------------
-                // The whole warp walks through the loop and one elected lane issues, so that descriptors and addresses
-                // are the warp's and stay in uniform registers.
-                const int ksteps = (a.dim + 15) >> 4;
-                const uint32_t idesc_pv = instr_desc<T>(16 * ksteps, true), idesc_qk = instr_desc<T>(0, false);
-                uint32_t slot = 0, tile = 0, items = 0;
-                uint32_t turns[2] = {0, 0}, weights[2] = {0, 0}, half_items[2] = {0, 0};  // scores issued, weights used
-                bool ok = true;
-                auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, tile_wait(bar, parity, a.status)); };
-                auto commit = [&](uint64_t* bar) {
-                    if (elect_one()) mma_commit(bar);
-                    __syncwarp();
-                };
-                auto full_wait = [&](uint32_t n) { wait(&sh->full[n % Shape::kStages], (n / Shape::kStages) & 1); };
-                auto slot_at = [&](uint32_t n) { return ring + (n % Shape::kStages) * Shape::kStageBytes; };
-                // S_h = Q_h K^T over keys [64 sub, 64 sub + keys) of the tile in k_slot
-                auto scores = [&](int h, uint32_t k_slot, int sub, int keys, int flags) {
-                    const int n = max(16, (keys + 15) & ~15);
-                    const uint32_t idesc = idesc_qk + ((uint32_t)(n >> 3) << 17), d = tmem + 128u * h + 64u * (turns[h] & 1);
-                    const uint32_t qa = desc_low(q_base + h * Shape::kStageBytes, 0), ka = desc_low(slot_at(k_slot) + 8192u * sub, 0);
-                    if (elect_one()) {
-#pragma unroll
-                        for (int k = 0; k < 4 * DB; ++k) {
-                            const uint32_t off = ((uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32u) >> 4;
-                            if (k < ksteps) mma_ss(d, desc_of(qa + off), desc_of(ka + off), idesc, k > 0);
-                        }
-                        sh->half_meta[h][turns[h] & 3] = keys | flags;
-                        mma_commit(&sh->s_full[h][turns[h] & 1]);
-                        mbar_arrive(&sh->s_full[h][turns[h] & 1]);
+        if (warp < 10) {
+            // ---------------- matrix instructions of one half ----------------
+            // The whole warp walks through the loop and one elected lane issues, so that descriptors and addresses are the
+            // warp's and stay in uniform registers.
+            const int h = warp - 8;
+            const int ksteps = (a.dim + 15) >> 4;
+            const uint32_t idesc_pv = instr_desc<T>(16 * ksteps, true), idesc_qk = instr_desc<T>(0, false);
+            const uint32_t s_at = tmem + 128u * h, o_at = tmem + 256u + 128u * h;
+            const uint32_t qa = desc_low(q_base + h * Shape::kStageBytes, 0);
+            uint32_t slot = 0, tile = 0, items = 0;             // ring slots, key tiles and items so far
+            uint32_t turns = 0, weights = 0, half_items = 0;    // scores issued, weights used, items with rows in this half
+            bool ok = true;
+            auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, tile_wait(bar, parity, a.status)); };
+            auto commit = [&](uint64_t* bar) {
+                if (elect_one()) mma_commit(bar);
+                __syncwarp();
+            };
+            auto full_wait = [&](uint32_t n) { wait(&sh->full[n % Shape::kStages], (n / Shape::kStages) & 1); };
+            auto slot_at = [&](uint32_t n) { return ring + (n % Shape::kStages) * Shape::kStageBytes; };
+            auto next_meta = [&]() { return __shfl_sync(0xffffffffu, sh->meta[tile++ & 15], 0); };
+            for (;;) {
+                wait(&sh->q_full, items & 1);
+                if (!ok) break;
+                const int rows = __shfl_sync(0xffffffffu, sh->info[items & 3].rows, 0), tag = (int)(items & 3) << kItemShift;
+                if (rows == 0) break;  // no more items
+                ++items;
+                if (rows <= h * kHalf) {  // nothing in this half: only give the places back
+                    if (elect_one()) mbar_arrive(&sh->q_empty);
+                    for (bool last = false; !last;) {
+                        full_wait(slot);
+                        if (!ok) break;
+                        last = next_meta() >> 16;
+                        if (elect_one()) mbar_arrive(&sh->empty[slot % Shape::kStages]);
+                        // (not before it is full: the arrival could count for the tile that lies there still)
+                        full_wait(slot + 1);
+                        if (!ok) break;
+                        if (elect_one()) mbar_arrive(&sh->empty[(slot + 1) % Shape::kStages]);
+                        __syncwarp();
+                        slot += 2;
                     }
-                    __syncwarp();
-                    ++turns[h];
-                };
+                    if (!ok) break;
+                    continue;
+                }
+                // One walk over the turns of the item: the scores of turn j + 1 are issued ahead of the products of turn j.
+                uint32_t k_slot = slot, v_slot = 0;
+                full_wait(k_slot);
+                if (!ok) break;
+                tmem_after_sync();
+                int k_meta = next_meta(), k_sub = 0, v_sub = 0, v_keys = 0;
+                bool more = true, first = true, start = true, v_frees = false;
                 for (;;) {
-                    wait(&sh->q_full, items & 1);
-                    if (!ok) break;
-                    const int rows = __shfl_sync(0xffffffffu, sh->info[items & 3].rows, 0);
-                    if (rows == 0) break;  // no more items
-                    const int halves = rows > kHalf ? 2 : 1, tag = (int)(items & 3) << kItemShift;
-                    // One walk over the turns of the item: the scores of turn j + 1 are issued ahead of the products
-                    // of turn j.  (k_slot, k_sub, k_keys): where the scores are; v_*: where the products are.
-                    uint32_t k_slot = slot;
-                    full_wait(k_slot);
-                    if (!ok) break;
-                    tmem_after_sync();
-                    int k_meta = __shfl_sync(0xffffffffu, sh->meta[tile & 15], 0), k_sub = 0;
-                    ++tile;
-                    bool more = true, first = true;
-                    int v_keys = 0, v_sub = 0;
-                    uint32_t v_slot = 0;
-                    bool v_frees = false;
-                    for (;;) {
-                        int keys = 0, sub = 0;
-                        uint32_t at = 0;
-                        bool frees = false;
-                        if (more) {
-                            const int left = (k_meta & 0xffff) - kSub * k_sub;
-                            keys = min(left, kSub);
-                            sub = k_sub;
-                            at = k_slot;
-                            frees = left <= kSub;  // the tile's last turn
-                            const bool last = frees && (k_meta >> 16);
-                            for (int h = 0; h < halves; ++h) scores(h, k_slot, sub, keys, (last ? kLast : 0) | tag);
-                            if (frees) {
-                                commit(&sh->empty[k_slot % Shape::kStages]);
-                                if (last) commit(&sh->q_empty);
-                            }
-                            more = !last;
-                            ++k_sub;
-                        }
-                        if (!first) {
-                            // O_h += P_h V over the turn before
-                            if (v_sub == 0) full_wait(v_slot);
-                            const bool start = v_slot == slot + 1 && v_sub == 0, stop = keys == 0 && !frees;
-                            const uint32_t va = desc_low(slot_at(v_slot) + 8192u * v_sub, kBlockBytes);
-                            const int steps = max(1, (v_keys + 15) >> 4);
-                            for (int h = 0; h < halves && ok; ++h) {
-                                wait(&sh->p_full[h][weights[h] & 1], (weights[h] >> 1) & 1);
-                                if (start) wait(&sh->o_empty[h], (half_items[h] & 1) ^ 1);
-                                if (!ok) break;
-                                tmem_after_sync();
-                                const uint32_t pa = tmem + 128u * h + 64u * (weights[h] & 1);
-                                if (elect_one()) {
+                    int keys = 0;
+                    const int sub = k_sub;
+                    const uint32_t at = k_slot;
+                    bool frees = false;
+                    if (more) {
+                        // S = Q K^T over the next keys
+                        const int left = (k_meta & 0xffff) - kSub * k_sub;
+                        keys = min(left, kSub);
+                        frees = left <= kSub;  // the tile's last turn
+                        const bool last = frees && (k_meta >> 16);
+                        const int n = max(16, (keys + 15) & ~15);
+                        const uint32_t idesc = idesc_qk + ((uint32_t)(n >> 3) << 17), d = s_at + 64u * (turns & 1);
+                        const uint32_t ka = desc_low(slot_at(k_slot) + 8192u * sub, 0);
+                        if (elect_one()) {
 #pragma unroll
-                                    for (int k = 0; k < 4; ++k)
-                                        if (k < steps)
-                                            mma_ts(tmem + 256u + 128u * h, pa + 8u * k, desc_of(va + 128u * k), idesc_pv, !start || k > 0);
-                                    mma_commit(&sh->pv_done[h][weights[h] & 1]);
-                                }
-                                __syncwarp();
-                                ++weights[h];
-                                if (stop) ++half_items[h];
+                            for (int k = 0; k < 4 * DB; ++k) {
+                                const uint32_t off = ((uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32u) >> 4;
+                                if (k < ksteps) mma_ss(d, desc_of(qa + off), desc_of(ka + off), idesc, k > 0);
                             }
-                            if (!ok) break;
-                            if (v_frees) commit(&sh->empty[v_slot % Shape::kStages]);
-                            if (stop) {
-                                slot = v_slot + 1;
-                                break;
-                            }
+                            sh->half_meta[h][turns & 3] = keys | (last ? kLast : 0) | tag;
+                            mma_commit(&sh->s_full[h][turns & 1]);
+                            mbar_arrive(&sh->s_full[h][turns & 1]);
+                            if (frees) mma_commit(&sh->empty[k_slot % Shape::kStages]);
+                            if (last) mma_commit(&sh->q_empty);
                         }
-                        first = false;
-                        v_keys = keys;
-                        v_sub = sub;
-                        v_slot = at + 1;
-                        v_frees = frees;
-                        if (more && frees) {  // on to the next tile's keys
-                            k_slot += 2;
-                            k_sub = 0;
-                            full_wait(k_slot);
-                            if (!ok) break;
-                            tmem_after_sync();
-                            k_meta = __shfl_sync(0xffffffffu, sh->meta[tile & 15], 0);
-                            ++tile;
-                        }
+                        __syncwarp();
+                        ++turns;
+                        more = !last;
+                        ++k_sub;
                     }
-                    if (!ok) break;
-                    ++items;
-                }
-                if (ok) {  // the softmax groups may leave
-                    if (elect_one()) {
+                    if (!first) {
+                        // O += P V over the turn before
+                        const bool stop = keys == 0 && !frees;
+                        const uint32_t va = desc_low(slot_at(v_slot) + 8192u * v_sub, kBlockBytes), pa = s_at + 64u * (weights & 1);
+                        const int steps = max(1, (v_keys + 15) >> 4);
+                        if (v_sub == 0) full_wait(v_slot);
+                        if (start) wait(&sh->o_empty[h], (half_items & 1) ^ 1);
+                        wait(&sh->p_full[h][weights & 1], (weights >> 1) & 1);
+                        if (!ok) break;
+                        tmem_after_sync();
+                        if (elect_one()) {
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            sh->half_meta[h][turns[h] & 3] = kStop;
-                            mbar_arrive(&sh->s_full[h][turns[h] & 1]);
-                            mbar_arrive(&sh->s_full[h][turns[h] & 1]);
+                            for (int k = 0; k < 4; ++k)
+                                if (k < steps) mma_ts(o_at, pa + 8u * k, desc_of(va + 128u * k), idesc_pv, !start || k > 0);
+                            mma_commit(&sh->pv_done[h][weights & 1]);
+                            if (v_frees) mma_commit(&sh->empty[v_slot % Shape::kStages]);
                         }
+                        __syncwarp();
+                        ++weights;
+                        start = false;
+                        if (stop) break;
                     }
-                    __syncwarp();
+                    first = false;
+                    v_keys = keys;
+                    v_sub = sub;
+                    v_slot = at + 1;
+                    v_frees = frees;
+                    if (more && frees) {  // on to the next tile's keys
+                        k_slot += 2;
+                        k_sub = 0;
+                        full_wait(k_slot);
+                        if (!ok) break;
+                        tmem_after_sync();
+                        k_meta = next_meta();
+                    }
                 }
-                commit(&sh->done);  // nothing of this CTA is under way when it gives its memory back
-                tile_wait(&sh->done, 0, a.status);
+                if (!ok) break;
+                slot = v_slot + 1;
+                ++half_items;
             }
+            if (ok) {  // the softmax group may leave
+                if (elect_one()) {
+                    sh->half_meta[h][turns & 3] = kStop;
+                    mbar_arrive(&sh->s_full[h][turns & 1]);
+                    mbar_arrive(&sh->s_full[h][turns & 1]);
+                }
+                __syncwarp();
+            }
+            commit(&sh->done[h]);  // nothing of this CTA is under way when it gives its memory back
+            tile_wait(&sh->done[h], 0, a.status);
         } else {
             // ---------------- loads ----------------
             Loader<DB> ld;
             ld.status = a.status;
             ld.lane = lane;
-            ld.warp = warp - 9;
+            ld.warp = warp - 10;
             ld.zero_row = static_cast<const char*>(a.q);
-            int* const list = sh->list[warp - 9];
+            int* const list = sh->list[warp - 10];
             ld.layout(2 * a.dim);
             uint32_t items = 0, tile = 0;
             for (int64_t w = blockIdx.x; w < total && !ld.dead; w += gridDim.x) {
@@ -680,19 +751,15 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                 auto load_queries = [&]() {
                     ld.wait(&sh->q_empty, (items & 1) ^ 1);
                     if (ld.dead) return;
-                    const int64_t row = 2 * a.q_row, head = 2 * a.q_head;
-                    const char* const q = static_cast<const char*>(a.q) + it.seg.q0 * row + (int64_t)it.kvh * a.group * head;
-                    for (int b = 0; b < it.rows; b += kHalf) {
-                        if (a.group == 1 && it.rows - b >= kHalf)
-                            ld.full_rows(q_base + (b / kHalf) * Shape::kStageBytes, q + (it.row0 + b) * row, row);
-                        else
-                            ld.rows(q_base + (b / kHalf) * Shape::kStageBytes, kHalf, [&](int r) -> const char* {
-                                int qrow, hd;
-                                tile_row(a, 0, it.row0 + b + r, qrow, hd);
-                                return b + r < it.rows ? q + qrow * row + hd * head : nullptr;
-                            });
-                    }
-                    if (warp == 9 && lane == 0) {
+                    const int row = (int)(2 * a.q_row), head = (int)(2 * a.q_head);
+                    const char* const q = static_cast<const char*>(a.q) + it.seg.q0 * 2 * a.q_row + (int64_t)it.kvh * a.group * 2 * a.q_head;
+                    for (int b = 0; b < it.rows; b += kHalf)
+                        ld.queries(q_base + (b / kHalf) * Shape::kStageBytes, [&](int r) -> const char* {
+                            int qrow, hd;
+                            tile_row(a, 0, it.row0 + b + r, qrow, hd);
+                            return b + r < it.rows ? q + (int64_t)qrow * row + (int64_t)hd * head : nullptr;
+                        });
+                    if (warp == 10 && lane == 0) {
                         TileInfo& info = sh->info[items & 3];
                         info.q0 = it.seg.q0;
                         info.work = w;
@@ -710,18 +777,20 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                 const char* const v = reinterpret_cast<const char*>(static_cast<const T*>(a.v) + it.seg.k0 * a.v_row + it.kvh * a.v_head);
                 const uint8_t* const mask = a.mask ? a.mask + it.seg.k0 : nullptr;
                 int cursor = it.kb, listed = 0;
+                bool seen[4];  // of the 128 keys from the cursor on, fetched ahead
+                auto look_ahead = [&]() {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int key = cursor + 32 * j + lane;
+                        seen[j] = key < it.ke && mask[key] != 0;
+                    }
+                };
+                if (mask) look_ahead();
                 for (bool last = false; !last && !ld.dead; ++tile) {
                     // the next 128 visible keys
                     int take, from = cursor;
                     if (mask) {
-                        while (listed <= kHalf && cursor < it.ke) {
-                            bool seen[4];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const int key = cursor + 32 * j + lane;
-                                seen[j] = key < it.ke && mask[key] != 0;
-                            }
-                            // (at most 128 are listed here, and 128 more fit)
+                        while (listed <= kHalf && cursor < it.ke) {  // (at most 128 are listed here, and 128 more fit)
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 const unsigned ballot = __ballot_sync(0xffffffffu, seen[j]);
@@ -729,6 +798,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                                 listed += __popc(ballot);
                             }
                             cursor += 128;
+                            look_ahead();
                         }
                         __syncwarp();
                         take = min(listed, kHalf);
@@ -738,22 +808,18 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                         cursor += take;
                         last = cursor >= it.ke;
                     }
-                    const int padded = max(16, (take + 15) & ~15);  // rows that the matrix instructions read
-                    if (warp == 9 && lane == 0) sh->meta[tile & 15] = take | (last ? 1 << 16 : 0);
+                    if (warp == 10 && lane == 0) sh->meta[tile & 15] = take | (last ? 1 << 16 : 0);
 #pragma unroll
                     for (int which = 0; which < 2; ++which) {
                         const uint32_t n = ld.slot;
                         ld.wait(&sh->empty[n % Shape::kStages], ((n / Shape::kStages) & 1) ^ 1);
                         if (ld.dead) break;
                         const char* const src = which ? v : k;
-                        const int64_t stride = 2 * (which ? a.v_row : a.k_row);
+                        const int stride = (int)(2 * (which ? a.v_row : a.k_row));
                         const uint32_t dst = ring + (n % Shape::kStages) * Shape::kStageBytes;
-                        if (mask)
-                            ld.rows(dst, padded, [&](int r) -> const char* { return r < take ? src + list[r] * stride : nullptr; });
-                        else if (take == kHalf)
-                            ld.full_rows(dst, src + from * stride, stride);
-                        else
-                            ld.rows(dst, padded, [&](int r) -> const char* { return r < take ? src + (from + r) * stride : nullptr; });
+                        if (mask) ld.tile(dst, take, src, stride, [&](int r) { return list[r]; });
+                        else if (take == kHalf) ld.full_tile(dst, src + (int64_t)from * stride, stride);
+                        else ld.tile(dst, take, src, stride, [&](int r) { return from + r; });
                         ld.issued(&sh->full[n % Shape::kStages]);
                         ++ld.slot;
                     }
@@ -778,7 +844,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
             if (!ld.dead) ld.wait(&sh->q_empty, (items & 1) ^ 1);
             ld.flush();
             if (!ld.dead) {  // an item without rows: there are no more
-                if (warp == 9 && lane == 0) sh->info[items & 3].rows = 0;
+                if (warp == 10 && lane == 0) sh->info[items & 3].rows = 0;
                 __syncwarp();
                 mbar_arrive(&sh->q_full);
             }
