@@ -8,16 +8,15 @@
 //   warps 8, 9       issue the matrix instructions of one half each: S_h = Q_h K^T, O_h += P_h V.  (One warp for both was
 //                    what the kernel waited for: its waits, about 150 clocks each though satisfied, left the tensor
 //                    cores idle for 40 % of the time.)
-//   warps 10, 11     fetch queries, keys and values with 16-byte asynchronous copies into shared memory, in the
+//   warps 10-13      fetch queries, keys and values with 16-byte asynchronous copies into shared memory, in the
 //                    128-byte swizzle that the matrix instructions read.  Copies by row (rather than by tensor
 //                    map) let a tile consist of the VISIBLE keys only, wherever they lie: hidden keys cost a byte
 //                    of mask and nothing else, and what they hold is never looked at.
 // Keys are fetched 128 at a time and worked on 64 at a time: tensor memory holds two score buffers per half (S0a S0b
 // S1a S1b, 64 columns each, then O0 and O1, 128 each), so that the scores of the next 64 keys are made while the
 // softmax works on these and a half never waits for the matrix instructions of its own weights.
-// A rescaling of O is rare: the reference that the exponents are taken against only follows the row's maximum
-// when it has grown by more than 2^8 (weights up to 2^8 lose nothing in binary32 sums or 16-bit weights); the
-// group then waits for the products under way and rescales O itself.
+// A rescaling of O is rare: the reference that the exponents are taken against only follows the row's maximum when the
+// weights have grown large (kMostInTurn); the group then waits for the products under way and rescales O itself.
 #include <math.h>
 
 #include "octo_attend.cuh"
@@ -25,15 +24,15 @@
 
 namespace octo {
 
-constexpr int kTileThreads = 384;
+constexpr int kTileThreads = 512;
 constexpr int kHalf = 128;            // rows of a half, keys of a tile
 constexpr int kSub = 64;              // keys of a turn
-constexpr int kLoadWarps = 2, kLoaders = 32 * kLoadWarps;
+constexpr int kLoadWarps = 4, kLoaders = 32 * kLoadWarps;
 constexpr int kBlockBytes = 128 * 128;  // 128 rows of 64 elements
 constexpr int kListInts = 256;
-constexpr float kSlack = 8.0f;        // growth of the maximum, as a power of two, before the reference has to follow
-constexpr float kMostInTurn = 1024.0f;  // sum of a turn's 64 weights up to which it does not
-constexpr float kGrown = 4.0f;          // (64 weights that sum to more than 1024: one is above 2^4)
+// The reference that exponents are taken against stays while a turn's 64 weights sum to no more than 2^10 (weights that
+// large lose nothing in binary32 sums, and fp16 holds them); where they sum to more, one of them is above 2^4.
+constexpr float kMostInTurn = 1024.0f, kGrown = 4.0f;
 
 template <int DB>
 struct TileShape {
@@ -127,57 +126,23 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
         "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::OCTO_W8(r, 0), OCTO_W8(r, 8), OCTO_W8(r, 16), OCTO_W8(r, 24), "r"(addr)
         : "memory");
 }
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float d;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-    return d;
-}
 __device__ __forceinline__ void halves_of(unsigned long long v, float& x, float& y) {
     asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
 }
 __device__ __forceinline__ unsigned long long pair_of(float v) { return f32x2(v, v); }
 
-// 2^x and 2^y on the multiply-add pipe, for x, y <= kSlack: x = n + f with n whole and |f| <= 1/2, a polynomial for 2^f (degree
-// 4, fitted to the least relative error on [-1/2, 1/2], 2.7e-6) and n added to its exponent.  Arguments below
-// -126 count as -126 (a weight that no sum keeps); NaN gives a number above 2^126 or NaN.
-__device__ __forceinline__ void ex2_by_polynomial(float& x, float& y) {
-    const unsigned long long magic = pair_of(12582912.0f);  // 1.5 * 2^23: adding it rounds to whole numbers
-    const unsigned long long v = f32x2(max_nan(x, -126.0f), max_nan(y, -126.0f));
-    const unsigned long long n = add_f32x2(v, magic);
-    const unsigned long long f = fma_f32x2(add_f32x2(n, pair_of(-12582912.0f)), pair_of(-1.0f), v);
-    unsigned long long q = fma_f32x2(f, pair_of(0x1.3997d4p-7f), pair_of(0x1.ca1440p-5f));
-    q = fma_f32x2(q, f, pair_of(0x1.ec06dap-3f));
-    q = fma_f32x2(q, f, pair_of(0x1.62e0dcp-1f));
-    q = fma_f32x2(q, f, pair_of(0x1.ffffe8p-1f));
-    float nx, ny;
-    halves_of(n, nx, ny);
-    halves_of(q, x, y);
-    x = __uint_as_float(__float_as_uint(x) + (__float_as_uint(nx) << 23));
-    y = __uint_as_float(__float_as_uint(y) + (__float_as_uint(ny) << 23));
-}
-
 // Weights of 32 scores: 2^(s * scale + minus), packed in the type of the values, and their sum (of the unrounded ones).
-// The special-function unit takes eight clocks for a warp's exponentials, and both halves' warps share it: without EXACT
-// every fourth pair goes to the multiply-add pipe instead.  `top`: the largest exponent among those.
-template <typename T, bool EXACT>
+// (A polynomial on the multiply-add pipe for every fourth pair, to relieve the special-function unit, cost more issue
+// slots than it freed: 2230 -> 2325 us over 64 segments of 1024 queries and 4096 keys, 16 heads of 128.)
+template <typename T>
 __device__ __forceinline__ void weigh(const uint32_t* s, unsigned long long scale, unsigned long long minus, uint32_t* p,
-                                      unsigned long long& sum, float& top) {
+                                      unsigned long long& sum) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         float x, y;
         halves_of(fma_f32x2(f32x2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale, minus), x, y);
-        if (!EXACT && false) {
-            top = max3(top, x, y);
-            ex2_by_polynomial(x, y);
-        } else {
-            x = ex2(x);
-            y = ex2(y);
-        }
+        x = ex2(x);
+        y = ex2(y);
         sum = add_f32x2(sum, f32x2(x, y));
         p[i] = pack2<T>(x, y);  // what the matrix instruction takes
     }
@@ -404,7 +369,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
 
     if (warp < 8) {
         // ---------------- softmax of one half ----------------
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
         const int h = warp >> 2, row = threadIdx.x & (kHalf - 1);
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);  // the warp's 32 lanes of tensor memory
         const uint32_t o_at = lanes + 256u + 128u * h;
@@ -419,8 +384,13 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
             float ref = -INFINITY, sum = 0.0f;  // what the exponents are taken against; sum of the weights
             bool look = true;    // the scores have to be looked through before they are weighed
             bool first = true, ahead = false;  // ahead: the turn's scores are on their way into s0 already
-            int meta = 0;
+            int meta = 0, next_meta = 0;
             uint32_t s0[32], s1[32], p[32];
+            auto hand_over = [&]() {
+                tmem_wait_st();
+                tmem_before_sync();
+                mbar_arrive(&sh->p_full[h][(turn - 1) & 1]);
+            };
             while (!(meta & (kLast | kStop))) {
                 if (!ahead) {
                     if (!__all_sync(0xffffffffu, tile_wait(&sh->s_full[h][turn & 1], (turn >> 1) & 1, a.status))) {
@@ -428,12 +398,14 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                         break;
                     }
                     tmem_after_sync();
+                    meta = sh->half_meta[h][turn & 3];
+                    if (meta & kStop) break;
+                    tmem_ld32(scores_at(turn), s0);
+                } else {
+                    meta = next_meta;
                 }
-                meta = sh->half_meta[h][turn & 3];
-                if (meta & kStop) break;
                 const int take = meta & 0xff;
                 const uint32_t s_at = scores_at(turn);
-                if (!ahead) tmem_ld32(s_at, s0);
                 tmem_landed(s0);
                 ahead = false;
                 unsigned long long part = 0ull;
@@ -441,25 +413,26 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                 if (!again) {
                     // Weights against the reference so far: the exponentials do not wait for a maximum.
                     const unsigned long long minus = pair_of(-ref);
-                    float top = -INFINITY;
                     tmem_ld32(s_at + 32, s1);
-                    weigh<T, false>(s0, sc2, minus, p, part, top);
+                    weigh<T>(s0, sc2, minus, p, part);
+                    const bool ready = !(meta & kLast) && mbar_test_wait(&sh->s_full[h][(turn + 1) & 1], ((turn + 1) >> 1) & 1);
                     tmem_landed(s1);
-                    // the next turn's scores are fetched beside this one's second half, if they are there
-                    if (!(meta & kLast) && __all_sync(0xffffffffu, mbar_test_wait(&sh->s_full[h][(turn + 1) & 1], ((turn + 1) >> 1) & 1))) {
+                    if (__all_sync(0xffffffffu, ready)) {
                         tmem_after_sync();
+                        // (read once the barrier is known to be through: a load beside its test was served before it)
+                        next_meta = *reinterpret_cast<volatile int*>(&sh->half_meta[h][(turn + 1) & 3]);
                         tmem_ld32(scores_at(turn + 1), s0);
                         ahead = true;
                     }
-                    weigh<T, false>(s1, sc2, minus, p + 16, part, top);
+                    weigh<T>(s1, sc2, minus, p + 16, part);
                     float x, y;
                     halves_of(part, x, y);
                     // A weight far above the reference shows in the sum (false for NaN: it comes through the weights).
-                    again = __any_sync(0xffffffffu, x + y > kMostInTurn || top > kSlack);
+                    again = __any_sync(0xffffffffu, x + y > kMostInTurn);
                 }
                 if (again) {
                     // The first turn, the last one where it is not full, and turns in which a row has outgrown its reference: the
-                    // scores, still in tensor memory, are looked through, the reference follows, and they are weighed exactly.
+                    // scores, still in tensor memory, are looked through, the reference follows, and they are weighed.
                     if (ahead) tmem_landed(s0);  // (taken once more below)
                     ahead = false;
                     const uint32_t none = __float_as_uint(sc < 0.0f ? INFINITY : -INFINITY);  // behind the last visible key
@@ -501,9 +474,9 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                     look = __any_sync(0xffffffffu, ref == -INFINITY);
                     const unsigned long long minus = pair_of(ref == -INFINITY ? 0.0f : -ref);
                     part = 0ull;
-                    weigh<T, true>(s0, sc2, minus, p, part, top);
+                    weigh<T>(s0, sc2, minus, p, part);
                     if (take > 32) {
-                        weigh<T, true>(s1, sc2, minus, p + 16, part, top);
+                        weigh<T>(s1, sc2, minus, p + 16, part);
                     } else {  // (the matrix instruction reads the first 32 weights then)
 #pragma unroll
                         for (int i = 16; i < 32; ++i) p[i] = 0u;
@@ -514,10 +487,8 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                 float x, y;
                 halves_of(part, x, y);
                 sum += x + y;
-                tmem_wait_st();
-                tmem_before_sync();
-                mbar_arrive(&sh->p_full[h][turn & 1]);
                 ++turn;
+                hand_over();
             }
             if (dead || (meta & kStop)) break;
             // the half's rows of the result
@@ -602,7 +573,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
             }
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         if (warp < 10) {
             // ---------------- matrix instructions of one half ----------------
             // The whole warp walks through the loop and one elected lane issues, so that descriptors and addresses are the
@@ -646,82 +617,89 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                     if (!ok) break;
                     continue;
                 }
-                // One walk over the turns of the item: the scores of turn j + 1 are issued ahead of the products of turn j.
-                uint32_t k_slot = slot, v_slot = 0;
-                full_wait(k_slot);
-                if (!ok) break;
-                tmem_after_sync();
-                int k_meta = next_meta(), k_sub = 0, v_sub = 0, v_keys = 0;
-                bool more = true, first = true, start = true, v_frees = false;
-                for (;;) {
-                    int keys = 0;
-                    const int sub = k_sub;
-                    const uint32_t at = k_slot;
-                    bool frees = false;
-                    if (more) {
-                        // S = Q K^T over the next keys
-                        const int left = (k_meta & 0xffff) - kSub * k_sub;
-                        keys = min(left, kSub);
-                        frees = left <= kSub;  // the tile's last turn
-                        const bool last = frees && (k_meta >> 16);
-                        const int n = max(16, (keys + 15) & ~15);
-                        const uint32_t idesc = idesc_qk + ((uint32_t)(n >> 3) << 17), d = s_at + 64u * (turns & 1);
-                        const uint32_t ka = desc_low(slot_at(k_slot) + 8192u * sub, 0);
-                        if (elect_one()) {
-#pragma unroll
-                            for (int k = 0; k < 4 * DB; ++k) {
-                                const uint32_t off = ((uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32u) >> 4;
-                                if (k < ksteps) mma_ss(d, desc_of(qa + off), desc_of(ka + off), idesc, k > 0);
-                            }
-                            sh->half_meta[h][turns & 3] = keys | (last ? kLast : 0) | tag;
-                            mma_commit(&sh->s_full[h][turns & 1]);
-                            mbar_arrive(&sh->s_full[h][turns & 1]);
-                            if (frees) mma_commit(&sh->empty[k_slot % Shape::kStages]);
-                            if (last) mma_commit(&sh->q_empty);
-                        }
-                        __syncwarp();
-                        ++turns;
-                        more = !last;
-                        ++k_sub;
-                    }
-                    if (!first) {
-                        // O += P V over the turn before
-                        const bool stop = keys == 0 && !frees;
-                        const uint32_t va = desc_low(slot_at(v_slot) + 8192u * v_sub, kBlockBytes), pa = s_at + 64u * (weights & 1);
-                        const int steps = max(1, (v_keys + 15) >> 4);
-                        if (v_sub == 0) full_wait(v_slot);
-                        if (start) wait(&sh->o_empty[h], (half_items & 1) ^ 1);
-                        wait(&sh->p_full[h][weights & 1], (weights >> 1) & 1);
-                        if (!ok) break;
-                        tmem_after_sync();
-                        if (elect_one()) {
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                if (k < steps) mma_ts(o_at, pa + 8u * k, desc_of(va + 128u * k), idesc_pv, !start || k > 0);
-                            mma_commit(&sh->pv_done[h][weights & 1]);
-                            if (v_frees) mma_commit(&sh->empty[v_slot % Shape::kStages]);
-                        }
-                        __syncwarp();
-                        ++weights;
-                        start = false;
-                        if (stop) break;
-                    }
-                    first = false;
-                    v_keys = keys;
-                    v_sub = sub;
-                    v_slot = at + 1;
-                    v_frees = frees;
-                    if (more && frees) {  // on to the next tile's keys
-                        k_slot += 2;
-                        k_sub = 0;
+                // The turns of the item in order; scores run two turns ahead of products, into the buffer that the products
+                // before them have just read.  From the arrival of a turn's weights to the next scores nothing is
+                // waited for: places of keys and values are seen to while the softmax works.
+                struct Turn {
+                    uint32_t k;       // descriptor of its keys
+                    uint32_t slot;    // of its keys; the values follow
+                    int sub, keys;
+                    bool frees, last; // the tile's last turn; the item's
+                };
+                uint32_t k_slot = slot;
+                int k_meta = 0, k_sub = 0;
+                auto prepare = [&](Turn& t) {
+                    if (k_sub == 0) {
                         full_wait(k_slot);
-                        if (!ok) break;
-                        tmem_after_sync();
+                        if (!ok) return;
                         k_meta = next_meta();
                     }
+                    const int left = (k_meta & 0xffff) - kSub * k_sub;
+                    t.k = desc_low(slot_at(k_slot) + 8192u * k_sub, 0);
+                    t.slot = k_slot;
+                    t.sub = k_sub;
+                    t.keys = min(left, kSub);
+                    t.frees = left <= kSub;
+                    t.last = t.frees && (k_meta >> 16);
+                    k_sub = t.frees ? 0 : k_sub + 1;
+                    if (t.frees) k_slot += 2;
+                };
+                auto scores = [&](const Turn& t) {  // S = Q K^T, by the elected lane
+                    const uint32_t idesc = idesc_qk + ((uint32_t)(max(16, (t.keys + 15) & ~15) >> 3) << 17), d = s_at + 64u * (turns & 1);
+#pragma unroll
+                    for (int k = 0; k < 4 * DB; ++k) {
+                        const uint32_t off = ((uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32u) >> 4;
+                        if (k < ksteps) mma_ss(d, desc_of(qa + off), desc_of(t.k + off), idesc, k > 0);
+                    }
+                    sh->half_meta[h][turns & 3] = t.keys | (t.last ? kLast : 0) | tag;
+                    mma_commit(&sh->s_full[h][turns & 1]);
+                    mbar_arrive(&sh->s_full[h][turns & 1]);
+                    if (t.frees) mma_commit(&sh->empty[t.slot % Shape::kStages]);
+                    if (t.last) mma_commit(&sh->q_empty);
+                };
+                Turn now, next, after;
+                prepare(now);
+                if (!ok) break;
+                tmem_after_sync();
+                if (elect_one()) scores(now);
+                __syncwarp();
+                ++turns;
+                next = now;
+                if (!now.last) {
+                    prepare(next);
+                    if (!ok) break;
+                    if (elect_one()) scores(next);
+                    __syncwarp();
+                    ++turns;
+                }
+                for (bool start = true;; start = false) {
+                    const bool more = !now.last && !next.last;
+                    after = next;
+                    if (more) prepare(after);
+                    if (now.sub == 0) full_wait(now.slot + 1);
+                    if (start) wait(&sh->o_empty[h], (half_items & 1) ^ 1);
+                    const uint32_t va = desc_low(slot_at(now.slot + 1) + 8192u * now.sub, kBlockBytes), pa = s_at + 64u * (weights & 1);
+                    const int steps = max(1, (now.keys + 15) >> 4);
+                    wait(&sh->p_full[h][weights & 1], (weights >> 1) & 1);
+                    if (!ok) break;
+                    tmem_after_sync();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)  // O += P V
+                            if (k < steps) mma_ts(o_at, pa + 8u * k, desc_of(va + 128u * k), idesc_pv, !start || k > 0);
+                        mma_commit(&sh->pv_done[h][weights & 1]);
+                        if (now.frees) mma_commit(&sh->empty[(now.slot + 1) % Shape::kStages]);
+                        if (more) scores(after);
+                    }
+                    __syncwarp();
+                    ++weights;
+                    if (more) ++turns;
+                    if (now.last) break;
+                    now = next;
+                    next = after;
                 }
                 if (!ok) break;
-                slot = v_slot + 1;
+                slot = k_slot;
                 ++half_items;
             }
             if (ok) {  // the softmax group may leave
@@ -734,7 +712,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
             }
             commit(&sh->done[h]);  // nothing of this CTA is under way when it gives its memory back
             tile_wait(&sh->done[h], 0, a.status);
-        } else {
+        } else if (warp < 10 + kLoadWarps) {
             // ---------------- loads ----------------
             Loader<DB> ld;
             ld.status = a.status;
