@@ -229,9 +229,9 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         getattr(lib, name).restype = ctypes.c_int
     lib.octo_patch_positions.argtypes = [i32, vp, i32, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp]
     lib.octo_stage_patch_positions.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp]
-    lib.octo_norm_rotate.argtypes = [ctypes.POINTER(Rotate), vp]
-    lib.octo_attend_workspace.argtypes = [ctypes.POINTER(Attend), ctypes.POINTER(ctypes.c_int64)]
-    lib.octo_cross_attention.argtypes = [ctypes.POINTER(Attend), vp, ctypes.c_int64, vp]
+    lib.octo_norm_rotate.argtypes = [vp, vp]  # (octo_rotate_t packed into bytes, or by reference)
+    lib.octo_attend_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_int64)]
+    lib.octo_cross_attention.argtypes = [vp, vp, ctypes.c_int64, vp]
     for name in ("octo_patch_positions", "octo_stage_patch_positions", "octo_norm_rotate", "octo_attend_workspace",
                  "octo_cross_attention"):
         getattr(lib, name).restype = ctypes.c_int

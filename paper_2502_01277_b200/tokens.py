@@ -7,49 +7,56 @@ tensors' device, or on `stream`; nothing synchronises, and a call may be capture
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Optional, Tuple
 
 from . import binding as B
 
-_DTYPES = {"torch.float16": B.OCTO_F16, "torch.bfloat16": B.OCTO_BF16, "torch.float32": B.OCTO_F32}
-_streams = {}
+# Marshalling is what a small call costs, so arguments are packed in one go (the layouts of octo_rotate_t and
+# octo_attend_t) and what can be looked up once is.
+_ROTATE = struct.Struct("@10iq" + "Pqq" * 4 + "6Pqff")
+_ATTEND = struct.Struct("@6i2q" + "Pqq" * 4 + "2P6qPffP")
+assert _ROTATE.size == ctypes.sizeof(B.Rotate) and _ATTEND.size == ctypes.sizeof(B.Attend)
+
+
+class _Torch:
+    """torch and what is asked of it in every call; filled by the first."""
+    module = None
+    types: dict = {}
+    streams: dict = {}
+
+
+def _torch():
+    if _Torch.module is None:
+        import torch
+        _Torch.types = {torch.float16: B.OCTO_F16, torch.bfloat16: B.OCTO_BF16, torch.float32: B.OCTO_F32}
+        _Torch.module = torch
+    return _Torch.module
 
 
 def _refuse(where: str, why: str):
     raise B.OctoError(B.OCTO_E_INVALID_ARG, f"{where} ({why})")
 
 
-def _need(ok: bool, where: str, why: str) -> None:
-    if not ok:
-        _refuse(where, why)
-
-
-def _stream_of(torch, device, stream) -> int:
+def _stream_of(device, stream) -> int:
     if stream is not None:
         return int(stream.cuda_stream)
-    get = _streams.get(device.index)
+    get = _Torch.streams.get(device.index)
     if get is None:
-        get = _streams[device.index] = B._stream_getter(torch, device)
+        get = _Torch.streams[device.index] = B._stream_getter(_torch(), device)
     return get()
 
 
-def _on_device(where, device, **tensors) -> None:
+def _on_device(where, device, *tensors) -> None:
     """Every tensor given lies on `device`: a pointer of another one would be read there."""
-    for name, t in tensors.items():
+    for t in tensors:
         if t is not None and t.device != device:
-            _refuse(where, f"{name} is on {t.device}, not on {device}")
-
-
-def _heads(t) -> B.Heads:
-    h = B.Heads()
-    h.d_data, h.row_stride, h.head_stride = t.data_ptr(), t.stride(0), t.stride(1)
-    return h
+            _refuse(where, f"a tensor is on {t.device}, not on {device}")
 
 
 def _int32_vector(where, name, t, count) -> None:
-    if t is not None:
-        _need(str(t.dtype) == "torch.int32" and t.dim() == 1 and t.numel() >= count and t.is_contiguous(), where,
-              f"{name} is not a contiguous int32 vector of at least {count}")
+    if t is not None and (t.dtype is not _Torch.module.int32 or t.dim() != 1 or t.shape[0] < count or t.stride(0) != 1):
+        _refuse(where, f"{name} is not a contiguous int32 vector of at least {count}")
 
 
 def patch_positions(items, slot: Tuple[int, int], patch: int, *, keep_aspect: bool = False, times=None, n_items=None,
@@ -59,32 +66,32 @@ def patch_positions(items, slot: Tuple[int, int], patch: int, *, keep_aspect: bo
     items: item table on the GPU, int32 [n, 8] or uint8 [n, 32]; slot: (width, height) of a crop; times: float32
     [frames] or None; n_items: int32 {packed, ...} on the GPU or None (all of them).  Returns (positions float32
     [n, patches, 3], visible uint8 [n, patches]); rows of items beyond n_items are not written."""
-    import torch
-    where = "patch_positions"
-    _need(items.is_cuda and items.dim() == 2 and items.is_contiguous()
-          and (items.dtype, items.shape[1]) in ((torch.int32, 8), (torch.uint8, 32)), where,
-          "items is not a contiguous CUDA tensor of item records")
+    t, where = _torch(), "patch_positions"
+    if not (items.is_cuda and items.dim() == 2 and items.is_contiguous()
+            and (items.dtype, items.shape[1]) in ((t.int32, 8), (t.uint8, 32))):
+        _refuse(where, "items is not a contiguous CUDA tensor of item records")
     n, (w, h) = items.shape[0], slot
-    _need(patch > 0 and w > 0 and h > 0 and w % patch == 0 and h % patch == 0, where, "the patch does not divide the slot")
+    if not (patch > 0 and w > 0 and h > 0 and w % patch == 0 and h % patch == 0):
+        _refuse(where, "the patch does not divide the slot")
     dev, patches = items.device, (w // patch) * (h // patch)
     if positions is None:
-        positions = torch.empty((n, patches, 3), dtype=torch.float32, device=dev)
+        positions = t.empty((n, patches, 3), dtype=t.float32, device=dev)
     if visible is None:
-        visible = torch.empty((n, patches), dtype=torch.uint8, device=dev)
-    _need(positions.dtype == torch.float32 and positions.is_contiguous() and positions.numel() == n * patches * 3, where,
-          "positions has another shape")
-    _need(visible.dtype == torch.uint8 and visible.is_contiguous() and visible.numel() == n * patches, where,
-          "visible has another shape")
-    _need(times is None or (times.dtype == torch.float32 and times.dim() == 1 and times.is_contiguous()), where,
-          "times is not a contiguous float32 vector")
+        visible = t.empty((n, patches), dtype=t.uint8, device=dev)
+    if positions.dtype is not t.float32 or not positions.is_contiguous() or positions.numel() != n * patches * 3:
+        _refuse(where, "positions has another shape")
+    if visible.dtype is not t.uint8 or not visible.is_contiguous() or visible.numel() != n * patches:
+        _refuse(where, "visible has another shape")
+    if times is not None and (times.dtype is not t.float32 or times.dim() != 1 or not times.is_contiguous()):
+        _refuse(where, "times is not a contiguous float32 vector")
     _int32_vector(where, "n_items", n_items, 1)
-    _on_device(where, dev, times=times, n_items=n_items, positions=positions, visible=visible)
+    _on_device(where, dev, times, n_items, positions, visible)
     # without times every frame number is one that exists
-    frames = (1 << 31) - 1 if times is None else times.numel()
+    frames = (1 << 31) - 1 if times is None else times.shape[0]
     rc = B.load_library().octo_patch_positions(
         dev.index, items.data_ptr(), n, None if n_items is None else n_items.data_ptr(), w, h, patch,
         1 if keep_aspect else 0, None if times is None else times.data_ptr(), frames, positions.data_ptr(),
-        visible.data_ptr(), _stream_of(torch, dev, stream))
+        visible.data_ptr(), _stream_of(dev, stream))
     if rc != B.OCTO_OK:
         raise B.OctoError(rc, "octo_patch_positions")
     return positions, visible
@@ -99,47 +106,53 @@ def norm_rotate(q, k, positions, freqs, axes, *, q_weight=None, k_weight=None, e
     freqs float32 [pairs], axes int32 [pairs]: pair i turns by positions[:, axes[i]] * freqs[i].  q_weight,
     k_weight: [dim] of q's type, or None for no norm.  n_items (int32 on the GPU): rows from n_items * item_rows
     on are left as they were.  out: (q_out, k_out), which may be (q, k).  Returns (q_out, k_out)."""
-    import torch
-    where = "norm_rotate"
-    _need(q.is_cuda and q.dim() == 3 and str(q.dtype) in _DTYPES, where, "q is not a CUDA tensor [rows, heads, dim]")
-    dev, (rows, heads, dim) = q.device, q.shape
-    kv = 0 if k is None else k.shape[1]
-    _need(k is None or (k.dim() == 3 and k.shape[0] == rows and k.shape[2] == dim and k.dtype == q.dtype), where,
-          "k does not fit q")
+    t, where = _torch(), "norm_rotate"
+    dtype, dev = q.dtype, q.device
+    code = _Torch.types.get(dtype)
+    if code is None or not q.is_cuda or q.dim() != 3:
+        _refuse(where, "q is not a CUDA tensor [rows, heads, dim]")
+    rows, heads, dim = q.shape
+    kv = 0
+    if k is not None:
+        if k.dim() != 3 or k.dtype is not dtype or k.shape[0] != rows or k.shape[2] != dim:
+            _refuse(where, "k does not fit q")
+        kv = k.shape[1]
     if out is None:
-        out = (torch.empty((rows, heads, dim), dtype=q.dtype, device=dev),
-               None if k is None else torch.empty((rows, kv, dim), dtype=q.dtype, device=dev))
+        out = (t.empty((rows, heads, dim), dtype=dtype, device=dev),
+               None if k is None else t.empty((rows, kv, dim), dtype=dtype, device=dev))
     q_out, k_out = out
-    for name, a, b in (("q", q, q_out), ("k", k, k_out)):
-        if a is None:
+    views = []
+    for x, y in ((q, q_out), (k, k_out)):
+        if x is None:
+            views += ((0, 0, 0), (0, 0, 0))
             continue
-        _need(b is not None and b.shape == a.shape and b.dtype == a.dtype, where, f"the output of {name} has another shape")
-        _need(dim == 1 or (a.stride(2) == 1 and b.stride(2) == 1), where, f"the elements of a head of {name} are apart")
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        _need(w is None or (w.shape == (dim,) and w.dtype == q.dtype and w.is_contiguous()), where,
-              f"{name} is not a contiguous vector [dim] of q's type")
-    _need(freqs.dim() == 1 and freqs.dtype == torch.float32 and freqs.is_contiguous(), where, "freqs is not a float32 vector")
-    pairs = freqs.numel()
+        if y is None or y.shape != x.shape or y.dtype is not dtype:
+            _refuse(where, "an output has another shape than its input")
+        (r0, h0, e0), (r1, h1, e1) = x.stride(), y.stride()
+        if e0 != 1 or e1 != 1:
+            _refuse(where, "the elements of a head are apart")
+        views += ((x.data_ptr(), r0, h0), (y.data_ptr(), r1, h1))
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dtype is not dtype or w.dim() != 1 or w.shape[0] != dim or w.stride(0) != 1):
+            _refuse(where, "a weight is not a contiguous vector [dim] of q's type")
+    if freqs.dim() != 1 or freqs.dtype is not t.float32 or not freqs.is_contiguous():
+        _refuse(where, "freqs is not a float32 vector")
+    pairs = freqs.shape[0]
     _int32_vector(where, "axes", axes, pairs)
     _int32_vector(where, "n_items", n_items, 1)
-    _need(positions.dim() == 2 and positions.shape[0] == rows and positions.is_contiguous()
-          and positions.dtype in (torch.float32, torch.int32), where, "positions is not a contiguous float32 or int32 [rows, axes]")
-    _on_device(where, dev, k=k, positions=positions, freqs=freqs, axes=axes, q_weight=q_weight, k_weight=k_weight,
-               n_items=n_items, q_out=q_out, k_out=k_out)
-    a = B.Rotate()
-    a.device, a.dtype, a.heads, a.kv_heads, a.head_dim, a.pairs = dev.index, _DTYPES[str(q.dtype)], heads, kv, dim, pairs
-    a.interleaved, a.num_axes = 1 if interleaved else 0, positions.shape[1]
-    a.positions_are_int = 1 if positions.dtype == torch.int32 else 0
-    a.rows, a.eps = rows, eps
-    a.q, a.q_out = _heads(q), _heads(q_out)
-    if k is not None:
-        a.k, a.k_out = _heads(k), _heads(k_out)
-    a.d_q_weight = None if q_weight is None else q_weight.data_ptr()
-    a.d_k_weight = None if k_weight is None else k_weight.data_ptr()
-    a.d_positions, a.d_freqs, a.d_axes = positions.data_ptr(), freqs.data_ptr(), axes.data_ptr()
-    if n_items is not None:
-        a.d_n_items, a.item_rows = n_items.data_ptr(), item_rows
-    rc = B.load_library().octo_norm_rotate(ctypes.byref(a), _stream_of(torch, dev, stream))
+    whole = positions.dtype is t.int32
+    if not (whole or positions.dtype is t.float32) or positions.dim() != 2 or positions.shape[0] != rows or not positions.is_contiguous():
+        _refuse(where, "positions is not a contiguous float32 or int32 [rows, axes]")
+    _on_device(where, dev, k, positions, freqs, axes, q_weight, k_weight, n_items, q_out, k_out)
+    try:
+        args = _ROTATE.pack(dev.index, code, heads, kv, dim, pairs, 1 if interleaved else 0, positions.shape[1], 1 if whole else 0,
+                            0, rows, *views[0], *views[2], *views[1], *views[3],
+                            0 if q_weight is None else q_weight.data_ptr(), 0 if k_weight is None else k_weight.data_ptr(),
+                            positions.data_ptr(), freqs.data_ptr(), axes.data_ptr(), 0 if n_items is None else n_items.data_ptr(),
+                            item_rows, eps, 0.0)
+    except (struct.error, OverflowError) as e:
+        _refuse(where, str(e))
+    rc = B.load_library().octo_norm_rotate(args, _stream_of(dev, stream))
     if rc != B.OCTO_OK:
         raise B.OctoError(rc, "octo_norm_rotate")
     return q_out, k_out
@@ -157,48 +170,54 @@ def cross_attention(q, k, v, segments: int, *, q_offsets=None, k_offsets=None, q
     is known (it lets the call split its work well); key_mask: uint8 or bool [k_total], 0 hides a key; scale:
     dim ** -0.5 unless given; status: uint32 or int32 [1] that collects OCTO_STATUS bits.  Rows of no segment are
     not written.  Returns out [q_total, heads, dim]."""
-    import torch
-    where = "cross_attention"
-    _need(q.is_cuda and q.dim() == 3 and q.dtype in (torch.float16, torch.bfloat16), where,
-          "q is not a float16 or bfloat16 CUDA tensor [rows, heads, dim]")
-    dev, (q_total, heads, dim) = q.device, q.shape
-    _need(k.dim() == 3 and k.shape == v.shape and k.shape[2] == dim and k.dtype == q.dtype and v.dtype == q.dtype, where,
-          "k and v do not fit q")
-    k_total, kv = k.shape[0], k.shape[1]
-    _need(kv > 0 and heads % kv == 0, where, "kv_heads does not divide heads")
+    t, where = _torch(), "cross_attention"
+    dtype, dev = q.dtype, q.device
+    if not q.is_cuda or q.dim() != 3 or dtype not in (t.float16, t.bfloat16):
+        _refuse(where, "q is not a float16 or bfloat16 CUDA tensor [rows, heads, dim]")
+    q_total, heads, dim = q.shape
+    if k.dim() != 3 or k.shape != v.shape or k.shape[2] != dim or k.dtype is not dtype or v.dtype is not dtype:
+        _refuse(where, "k and v do not fit q")
+    k_total, kv, _ = k.shape
+    if kv == 0 or heads % kv:
+        _refuse(where, "kv_heads does not divide heads")
     if out is None:
-        out = torch.empty((q_total, heads, dim), dtype=q.dtype, device=dev)
-    _need(out.shape == q.shape and out.dtype == q.dtype, where, "out has another shape")
-    for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
-        _need(dim == 1 or t.stride(2) == 1, where, f"the elements of a head of {name} are apart")
+        out = t.empty((q_total, heads, dim), dtype=dtype, device=dev)
+    elif out.shape != q.shape or out.dtype is not dtype:
+        _refuse(where, "out has another shape")
+    views = []
+    for x in (q, k, v, out):
+        r, h, e = x.stride()
+        if e != 1:
+            _refuse(where, "the elements of a head are apart")
+        # (the strides of a dimension of one or of none mean nothing)
+        views += (x.data_ptr(), r if x.shape[0] > 1 else 0, h if x.shape[1] > 1 else 0)
     _int32_vector(where, "q_offsets", q_offsets, segments + 1)
     _int32_vector(where, "k_offsets", k_offsets, segments + 1)
-    _need(key_mask is None or (key_mask.dtype in (torch.uint8, torch.bool) and key_mask.shape == (k_total,)
-                               and key_mask.is_contiguous()), where, "key_mask is not a contiguous uint8 or bool [k_total]")
-    _need(status is None or (status.element_size() == 4 and status.numel() >= 1), where, "status is not a 32-bit word")
-    _on_device(where, dev, k=k, v=v, out=out, q_offsets=q_offsets, k_offsets=k_offsets, key_mask=key_mask, status=status)
-    a = B.Attend()
-    a.device, a.dtype, a.segments, a.heads, a.kv_heads, a.head_dim = dev.index, _DTYPES[str(q.dtype)], segments, heads, kv, dim
-    a.q_total, a.k_total = q_total, k_total
-    a.q, a.k, a.v, a.out = _heads(q), _heads(k), _heads(v), _heads(out)
-    a.d_q_offsets = None if q_offsets is None else q_offsets.data_ptr()
-    a.d_k_offsets = None if k_offsets is None else k_offsets.data_ptr()
-    a.q_rows, a.k_rows, a.q_first, a.k_first = q_rows, k_rows, q_first, k_first
-    a.max_q, a.max_k = max_q or 0, max_k or 0
-    a.d_key_mask = None if key_mask is None else key_mask.data_ptr()
-    a.scale = dim ** -0.5 if scale is None else scale
-    a.d_status = None if status is None else status.data_ptr()
-    lib, raw = B.load_library(), _stream_of(torch, dev, stream)
-    need = ctypes.c_int64(0)
-    rc = lib.octo_attend_workspace(ctypes.byref(a), ctypes.byref(need))
+    if key_mask is not None and (key_mask.dtype not in (t.uint8, t.bool) or key_mask.dim() != 1 or key_mask.shape[0] != k_total
+                                 or not key_mask.is_contiguous()):
+        _refuse(where, "key_mask is not a contiguous uint8 or bool [k_total]")
+    if status is not None and (status.element_size() != 4 or status.numel() < 1):
+        _refuse(where, "status is not a 32-bit word")
+    _on_device(where, dev, k, v, out, q_offsets, k_offsets, key_mask, status)
+    try:
+        args = _ATTEND.pack(dev.index, _Torch.types[dtype], segments, heads, kv, dim, q_total, k_total, *views,
+                            0 if q_offsets is None else q_offsets.data_ptr(), 0 if k_offsets is None else k_offsets.data_ptr(),
+                            q_rows, k_rows, q_first, k_first, max_q or 0, max_k or 0,
+                            0 if key_mask is None else key_mask.data_ptr(), dim ** -0.5 if scale is None else scale, 0.0,
+                            0 if status is None else status.data_ptr())
+    except (struct.error, OverflowError) as e:
+        _refuse(where, str(e))
+    lib = B.load_library()
+    need = ctypes.c_int64()
+    rc = lib.octo_attend_workspace(args, ctypes.byref(need))
     if rc != B.OCTO_OK:
         raise B.OctoError(rc, "octo_attend_workspace")
     workspace = None
     if need.value:
-        workspace = torch.empty((need.value,), dtype=torch.uint8, device=dev)
+        workspace = t.empty((need.value,), dtype=t.uint8, device=dev)
         if stream is not None:
             workspace.record_stream(stream)
-    rc = lib.octo_cross_attention(ctypes.byref(a), None if workspace is None else workspace.data_ptr(), need.value, raw)
+    rc = lib.octo_cross_attention(args, None if workspace is None else workspace.data_ptr(), need.value, _stream_of(dev, stream))
     if rc != B.OCTO_OK:
         raise B.OctoError(rc, "octo_cross_attention")
     return out
