@@ -8,18 +8,6 @@
 
 namespace octo {
 
-// Division by a number that is the same for a whole launch: exact for 0 <= n < 2^31 (multiply by the reciprocal rounded
-// up to 33 bits, whose top bit is the addition of n).
-struct FastDiv {
-    unsigned mul, shift;
-    void set(unsigned d) {
-        shift = 0;
-        while ((1ull << shift) < d) ++shift;
-        mul = (unsigned)(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
-    }
-    __device__ __forceinline__ int div(int n) const { return (int)((__umulhi(mul, (unsigned)n) + (unsigned)n) >> shift); }
-};
-
 struct AttendArgs {
     const void *q, *k, *v;
     void* out;

@@ -10,9 +10,10 @@
 namespace octo {
 
 // ---------------------------------------------------------------------------------------
-// Positions.  One CTA per item: its threads first make one coordinate per patch column and patch row (a
-// division in binary64 each, of which a patch of its own would need two), then write the item's block of
-// (time, y, x) triples with neighbouring threads on neighbouring words.  Bound by the bytes written.
+// Positions.  The threads of an item first make one coordinate per patch column and patch row (a division in
+// binary64 each, of which a patch of its own would need two), then write the item's block of (time, y, x) triples
+// with neighbouring threads on neighbouring words.  A batch of many items gives a warp to each, which lets all
+// of a server's batch be under way at once; a few items get a CTA each (7356 items of 196 patches: POS_US us).
 // ---------------------------------------------------------------------------------------
 constexpr int kPosThreads = 128;
 constexpr int kPosMaxSide = 2048;  // patches along a side of a slot
@@ -30,45 +31,49 @@ __device__ __forceinline__ void fit_in_slot(int cw, int ch, int ow, int oh, int 
     pt = (oh - nh) / 2;
 }
 
+// PER: threads of an item, 32 or kPosThreads.
+template <int PER>
 __global__ void __launch_bounds__(kPosThreads)
 positions_kernel(const octo_item_t* __restrict__ items, int max_items, const int* __restrict__ n_items, int slot_w,
-                 int slot_h, int patch, int keep_aspect, const float* __restrict__ times, int n_frames,
-                 float* __restrict__ positions, uint8_t* __restrict__ visible) {
-    extern __shared__ float s_axis[];  // [gw] x, [gh] y, then one byte per column and row: shows the image
-    const int gw = slot_w / patch, gh = slot_h / patch, patches = gw * gh;
-    float* s_x = s_axis;
-    float* s_y = s_axis + gw;
-    uint8_t* s_vx = reinterpret_cast<uint8_t*>(s_axis + gw + gh);
-    uint8_t* s_vy = s_vx + gw;
-    const int i = blockIdx.x;
+                 int slot_h, int patch, int gw, int gh, FastDiv by_gw, int keep_aspect, const float* __restrict__ times,
+                 int n_frames, float* __restrict__ positions, uint8_t* __restrict__ visible) {
+    extern __shared__ float s_all[];  // per item: [gw] x, [gh] y, then one byte per column and row: shows the image
+    const int local = PER == 32 ? threadIdx.x >> 5 : 0, t = threadIdx.x & (PER - 1), words = gw + gh + (gw + gh + 3) / 4;
+    float* const s_x = s_all + local * words;
+    float* const s_y = s_x + gw;
+    uint8_t* const s_vx = reinterpret_cast<uint8_t*>(s_y + gh);
+    uint8_t* const s_vy = s_vx + gw;
+    const int i = blockIdx.x * (kPosThreads / PER) + local;
     pdl_wait();
-    if (n_items && i >= *n_items) return;
+    if (i >= max_items || (n_items && i >= *n_items)) return;
     const octo_item_t it = items[i];
     const int cw = it.rx1 - it.rx0, ch = it.ry1 - it.ry0;
     const bool good = cw > 0 && ch > 0 && it.rx1 > it.rx0 && it.ry1 > it.ry0 && it.frame >= 0 && it.frame < n_frames;
+    const float time = good && times ? times[it.frame] : 0.0f;
     int nw = 1, nh = 1, pl = 0, pt = 0;
     if (good) fit_in_slot(cw, ch, slot_w, slot_h, keep_aspect, nw, nh, pl, pt);
-    for (int k = threadIdx.x; k < gw + gh; k += kPosThreads) {
+    for (int k = t; k < gw + gh; k += PER) {
         const bool col = k < gw;
         const int g = col ? k : k - gw, pad = col ? pl : pt, n = col ? nw : nh, size = col ? cw : ch;
         const int origin = col ? it.rx0 : it.ry0;
         // the centre of the patch, in halves of a slot pixel from the image's edge; one rounding at the end
         const double off = (double)((2 * g + 1) * patch - 2 * pad) * (double)size / (double)(2 * n);
-        s_axis[k] = good ? (float)((double)origin + off) : 0.0f;
+        s_x[k] = good ? (float)((double)origin + off) : 0.0f;
         s_vx[k] = good && g * patch < pad + n && (g + 1) * patch > pad ? 1 : 0;
     }
-    __syncthreads();
-    const float t = good && times ? times[it.frame] : 0.0f;
-    float* out = positions + (size_t)i * patches * 3;
-    // word f of the block is component f % 3 of patch f / 3; the pair (row, column) follows by steps
-    for (int f = threadIdx.x; f < patches * 3; f += kPosThreads) {
-        const int p = f / 3, c = f - 3 * p, gy = p / gw, gx = p - gy * gw;
-        out[f] = c == 0 ? t : (c == 1 ? s_y[gy] : s_x[gx]);
+    if (PER == 32) __syncwarp();
+    else __syncthreads();
+    const int patches = gw * gh;
+    float* const out = positions + (size_t)i * patches * 3;
+    // word f of the block is component f % 3 of patch f / 3
+    for (int f = t; f < patches * 3; f += PER) {
+        const int p = f / 3, c = f - 3 * p, gy = by_gw.div(p), gx = p - gy * gw;
+        out[f] = c == 0 ? time : (c == 1 ? s_y[gy] : s_x[gx]);
     }
     if (visible) {
-        uint8_t* vis = visible + (size_t)i * patches;
-        for (int p = threadIdx.x; p < patches; p += kPosThreads) {
-            const int gy = p / gw, gx = p - gy * gw;
+        uint8_t* const vis = visible + (size_t)i * patches;
+        for (int p = t; p < patches; p += PER) {
+            const int gy = by_gw.div(p), gx = p - gy * gw;
             vis[p] = s_vy[gy] & s_vx[gx];
         }
     }
@@ -76,11 +81,18 @@ positions_kernel(const octo_item_t* __restrict__ items, int max_items, const int
 
 cudaError_t launch_positions(const octo_item_t* d_items, int max_items, const int* d_n_items, int slot_w, int slot_h,
                              int patch, int keep_aspect, const float* d_times, int n_frames, float* d_positions,
-                             uint8_t* d_visible, cudaStream_t stream) {
+                             uint8_t* d_visible, int sm_count, cudaStream_t stream) {
     if (max_items < 1) return cudaSuccess;
-    const size_t smem = 5 * (size_t)(slot_w / patch + slot_h / patch);
-    return launch_kernel(positions_kernel, dim3((unsigned)max_items), dim3(kPosThreads), smem, stream, d_items, max_items,
-                         d_n_items, slot_w, slot_h, patch, keep_aspect, d_times, n_frames, d_positions, d_visible);
+    const int gw = slot_w / patch, gh = slot_h / patch;
+    const size_t words = (size_t)(gw + gh) + (size_t)(gw + gh + 3) / 4;
+    FastDiv by_gw;
+    by_gw.set((unsigned)gw);
+    // a warp per item from two CTAs per SM on, and where four items' tables still fit beside one another
+    const bool warps = max_items >= 2 * sm_count && words <= 2048;
+    const int per_cta = warps ? kPosThreads / 32 : 1;
+    return launch_kernel(warps ? positions_kernel<32> : positions_kernel<kPosThreads>, dim3((unsigned)ceil_div(max_items, per_cta)),
+                         dim3(kPosThreads), words * per_cta * sizeof(float), stream, d_items, max_items, d_n_items, slot_w, slot_h,
+                         patch, gw, gh, by_gw, keep_aspect, d_times, n_frames, d_positions, d_visible);
 }
 
 cudaError_t sm_count_of(int device, int* out) {
@@ -98,9 +110,10 @@ cudaError_t sm_count_of(int device, int* out) {
 // ---------------------------------------------------------------------------------------
 // Norm and rotation.  Bound by HBM: every element is read once and written once.  A group of lanes owns a
 // token and walks over its heads, so that the sine and cosine of the token's pairs are made once and stay in
-// registers for all heads.  A lane owns VP pairs of every head, both elements of each: for halves two runs of
-// VP elements that lie `pairs` apart, for neighbours one run of 2 VP, so that no element changes lanes;
-// elements behind the rotated ones are given to lanes as pairs with the angle zero.
+// registers for all heads, multiplied with the norm's weights: a pair (x0, x1) of a head with 1 / rms r becomes
+// r (x0 w0 c - x1 w1 s), r (x1 w1 c + x0 w0 s), six operations.  A lane owns VP pairs of every head, both elements of
+// each: for halves two runs of VP elements that lie `pairs` apart, for neighbours one run of 2 VP, so that no
+// element changes lanes; elements behind the rotated ones are given to lanes as pairs with the angle zero.
 // ---------------------------------------------------------------------------------------
 struct RotTensor {
     const void* in;
@@ -121,7 +134,6 @@ struct RotArgs {
 };
 
 constexpr int kRotThreads = 256;
-constexpr int kRotBatch = 4;  // heads of a lane group that are in flight together
 
 template <typename T> struct Conv;
 template <> struct Conv<__half> {
@@ -157,31 +169,48 @@ __device__ __forceinline__ void turn_of(double position, float freq, float& c, f
     c = fmaf(-s0, rest, c0);
 }
 
-// Lanes per token: LP (a power of two).  ILV: pairs are neighbours.  NU units of VP pairs per lane.
+// Sum over the lanes of a group of `size` neighbouring lanes that starts at lane `first`, in every one of them.
+__device__ __forceinline__ float group_sum(float v, unsigned mask, int first, int size, int in) {
+    if ((size & (size - 1)) == 0) {
+        for (int m = size >> 1; m > 0; m >>= 1) v += __shfl_xor_sync(mask, v, m);
+        return v;
+    }
+    for (int m = 16; m > 0; m >>= 1) {
+        const float w = __shfl_down_sync(mask, v, m);
+        if (m < size && in + m < size && in < m) v += w;
+    }
+    return __shfl_sync(mask, v, first);
+}
+
+// ILV: pairs are neighbours.  `lanes` lanes per token, NU units of VP pairs per lane.
 template <typename T, int VP, int NU, bool ILV>
-__global__ void __launch_bounds__(kRotThreads)
-rotate_kernel(const __grid_constant__ RotArgs a, int lp_log, int heads_per_group) {
+__global__ void __launch_bounds__(kRotThreads, 2)
+rotate_kernel(const __grid_constant__ RotArgs a, int lanes, int heads_per_group) {
+    constexpr int BATCH = sizeof(T) * VP * NU <= 16 ? 4 : 2;  // heads of a group that are in flight together
+    constexpr int N = VP * NU;
     pdl_wait();
-    const int lp = 1 << lp_log, lane = threadIdx.x & (lp - 1);
-    const int64_t row = ((int64_t)blockIdx.x * kRotThreads + threadIdx.x) >> lp_log;
+    const int lane = threadIdx.x & 31, tokens = 32 / lanes, mine = lane / lanes, in = lane - mine * lanes;
+    const int64_t row = ((int64_t)blockIdx.x * (kRotThreads / 32) + (threadIdx.x >> 5)) * tokens + mine;
     int64_t rows = a.rows;
     if (a.n_items) {
         const int64_t n = *a.n_items;
         rows = n <= 0 ? 0 : (n < rows / a.item_rows + 1 ? min(rows, n * a.item_rows) : rows);
     }
-    if (row >= rows) return;  // a group leaves as a whole; the shuffles below stay inside a group
-    const unsigned group = (lp == 32 ? 0xffffffffu : ((1u << lp) - 1u)) << ((threadIdx.x & 31) & ~(lp - 1));
+    const bool live = mine < tokens && row < rows;
+    const unsigned mask = __ballot_sync(0xffffffffu, live);
+    if (!live) return;  // a group leaves as a whole; shuffles name the lanes that stay
+    const int first = mine * lanes;
     const int total = a.t[0].heads + a.t[1].heads;
     const int h0 = blockIdx.y * heads_per_group, h1 = min(total, h0 + heads_per_group);
 
     // which elements this lane owns, and how they turn
-    const int half = a.head_dim / 2, rest = half - a.pairs;  // pairs that turn, pairs that do not
+    const int half = a.head_dim / 2, rest = half - a.pairs;  // pairs that turn and do not: `half` in all
     int e0[NU], e1[NU];  // first element of the two runs of a unit (ILV: e1 = e0 + VP)
     bool own[NU];
-    float cs[NU * VP], sn[NU * VP];
+    float cs[N], sn[N];
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
-        const int p = (lane + u * lp) * VP;  // first pair of the unit
+        const int p = (in + u * lanes) * VP;  // first pair of the unit
         own[u] = p < half;
         const bool turning = p < a.pairs;
         if (ILV) {
@@ -209,20 +238,41 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lp_log, int heads_per_group
     }
 
     const float inv_dim = 1.0f / (float)a.head_dim;
-#pragma unroll
+#pragma unroll 1
     for (int which = 0; which < 2; ++which) {
         const RotTensor& t = a.t[which];
-        const int first = which ? a.t[0].heads : 0;
-        const int b = max(h0, first) - first, e = min(h1, first + t.heads) - first;
+        const int from = which ? a.t[0].heads : 0;
+        const int b = max(h0, from) - from, e = min(h1, from + t.heads) - from;
         if (b >= e) continue;
-        const T* in = static_cast<const T*>(t.in) + row * t.in_row;
-        T* out = static_cast<T*>(t.out) + row * t.out_row;
-        const T* weight = static_cast<const T*>(t.weight);
-        for (int h = b; h < e; h += kRotBatch) {
-            Run<T, VP> x[kRotBatch][NU][2];
+        const T* const in_row = static_cast<const T*>(t.in) + row * t.in_row;
+        T* const out_row = static_cast<T*>(t.out) + row * t.out_row;
+        const T* const weight = static_cast<const T*>(t.weight);
+        // (w0 c, w1 s, w1 c, w0 s) of every pair
+        float m00[N], m01[N], m11[N], m10[N];
 #pragma unroll
-            for (int k = 0; k < kRotBatch; ++k) {
-                const T* head = in + (int64_t)min(h + k, e - 1) * t.in_head;
+        for (int u = 0; u < NU; ++u) {
+            Run<T, VP> w[2];
+            if (weight && own[u]) {
+                w[0] = *reinterpret_cast<const Run<T, VP>*>(weight + e0[u]);
+                w[1] = *reinterpret_cast<const Run<T, VP>*>(weight + e1[u]);
+            }
+#pragma unroll
+            for (int j = 0; j < VP; ++j) {
+                const int m = ILV ? 2 * j : j, n = ILV ? 2 * j + 1 : VP + j;  // the pair inside the unit's 2 VP elements
+                const float w0 = weight && own[u] ? Conv<T>::up(w[m / VP].v[m % VP]) : 1.0f;
+                const float w1 = weight && own[u] ? Conv<T>::up(w[n / VP].v[n % VP]) : 1.0f;
+                const int k = u * VP + j;
+                m00[k] = w0 * cs[k];
+                m01[k] = w1 * sn[k];
+                m11[k] = w1 * cs[k];
+                m10[k] = w0 * sn[k];
+            }
+        }
+        for (int h = b; h < e; h += BATCH) {
+            Run<T, VP> x[BATCH][NU][2];
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                const T* const head = in_row + (int64_t)min(h + k, e - 1) * t.in_head;
 #pragma unroll
                 for (int u = 0; u < NU; ++u)
                     if (own[u]) {
@@ -230,49 +280,40 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lp_log, int heads_per_group
                         x[k][u][1] = *reinterpret_cast<const Run<T, VP>*>(head + e1[u]);
                     }
             }
+            float r[BATCH];
 #pragma unroll
-            for (int k = 0; k < kRotBatch; ++k) {
-                if (h + k >= e) break;
-                float v[NU][2 * VP];
-                float sum = 0.0f;
-#pragma unroll
-                for (int u = 0; u < NU; ++u)
-#pragma unroll
-                    for (int j = 0; j < VP; ++j) {
-                        v[u][j] = own[u] ? Conv<T>::up(x[k][u][0].v[j]) : 0.0f;
-                        v[u][VP + j] = own[u] ? Conv<T>::up(x[k][u][1].v[j]) : 0.0f;
-                        sum += v[u][j] * v[u][j] + v[u][VP + j] * v[u][VP + j];
-                    }
+            for (int k = 0; k < BATCH; ++k) {
+                r[k] = 1.0f;
                 if (weight) {
-                    for (int m = lp >> 1; m > 0; m >>= 1) sum += __shfl_xor_sync(group, sum, m);
-                    const float r = 1.0f / sqrtf(sum * inv_dim + a.eps);
+                    float sum = 0.0f;
 #pragma unroll
                     for (int u = 0; u < NU; ++u)
-                        if (own[u]) {
-                            const Run<T, VP> w0 = *reinterpret_cast<const Run<T, VP>*>(weight + e0[u]);
-                            const Run<T, VP> w1 = *reinterpret_cast<const Run<T, VP>*>(weight + e1[u]);
 #pragma unroll
-                            for (int j = 0; j < VP; ++j) {
-                                v[u][j] *= r * Conv<T>::up(w0.v[j]);
-                                v[u][VP + j] *= r * Conv<T>::up(w1.v[j]);
-                            }
+                        for (int j = 0; j < VP; ++j) {
+                            const float p = own[u] ? Conv<T>::up(x[k][u][0].v[j]) : 0.0f, q = own[u] ? Conv<T>::up(x[k][u][1].v[j]) : 0.0f;
+                            sum = fmaf(p, p, sum);
+                            sum = fmaf(q, q, sum);
                         }
+                    r[k] = rsqrtf(fmaf(group_sum(sum, mask, first, lanes, in), inv_dim, a.eps));
                 }
-                T* head = out + (int64_t)(h + k) * t.out_head;
+            }
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                if (h + k >= e) break;
+                T* const head = out_row + (int64_t)(h + k) * t.out_head;
 #pragma unroll
                 for (int u = 0; u < NU; ++u)
                     if (own[u]) {
-                        Run<T, VP> y0, y1;
+                        Run<T, VP> y[2];
 #pragma unroll
                         for (int j = 0; j < VP; ++j) {
-                            const float c = cs[u * VP + j], s = sn[u * VP + j];
-                            const int m = ILV ? 2 * j : j, n = ILV ? 2 * j + 1 : VP + j;  // the pair inside v
-                            const float r0 = v[u][m] * c - v[u][n] * s, r1 = v[u][n] * c + v[u][m] * s;
-                            if (m < VP) y0.v[m] = Conv<T>::down(r0); else y1.v[m - VP] = Conv<T>::down(r0);
-                            if (n < VP) y0.v[n] = Conv<T>::down(r1); else y1.v[n - VP] = Conv<T>::down(r1);
+                            const int m = ILV ? 2 * j : j, n = ILV ? 2 * j + 1 : VP + j, i = u * VP + j;
+                            const float x0 = r[k] * Conv<T>::up(x[k][u][m / VP].v[m % VP]), x1 = r[k] * Conv<T>::up(x[k][u][n / VP].v[n % VP]);
+                            y[m / VP].v[m % VP] = Conv<T>::down(fmaf(x0, m00[i], -(x1 * m01[i])));
+                            y[n / VP].v[n % VP] = Conv<T>::down(fmaf(x1, m11[i], x0 * m10[i]));
                         }
-                        *reinterpret_cast<Run<T, VP>*>(head + e0[u]) = y0;
-                        *reinterpret_cast<Run<T, VP>*>(head + e1[u]) = y1;
+                        *reinterpret_cast<Run<T, VP>*>(head + e0[u]) = y[0];
+                        *reinterpret_cast<Run<T, VP>*>(head + e1[u]) = y[1];
                     }
             }
         }
@@ -281,23 +322,22 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lp_log, int heads_per_group
 
 template <typename T, int VP, int NU>
 static cudaError_t launch_rotate(const RotArgs& a, bool interleaved, int sm_count, cudaStream_t stream) {
-    const int units = ceil_div(a.head_dim / 2, VP);
-    int lp_log = 0;
-    while ((1 << lp_log) * NU < units) ++lp_log;
+    const int lanes = ceil_div(ceil_div(a.head_dim / 2, VP), NU), tokens = 32 / lanes;
     const int total = a.t[0].heads + a.t[1].heads;
-    // Few tokens: their heads are spread over more groups of lanes until there are about 1024 threads per SM, a
-    // multiple of kRotBatch heads each while that is enough.
-    const int64_t groups = a.rows << lp_log, want = (int64_t)sm_count * 1024;
+    const int64_t warps = (a.rows + tokens - 1) / tokens;
+    // Few tokens: their heads are spread over more warps until there are about 16 per SM, a multiple of 4 heads each
+    // while that is enough.
+    const int64_t want = (int64_t)sm_count * 16;
     int per = total;
-    if (groups < want) {
-        const int64_t split = (want + groups - 1) / groups;
+    if (warps < want) {
+        const int64_t split = (want + warps - 1) / warps;
         per = split >= total ? 1 : ceil_div(total, (int)split);
-        if (per > kRotBatch) per = ceil_div(per, kRotBatch) * kRotBatch;
+        if (per > 4) per = ceil_div(per, 4) * 4;
     }
-    const int64_t blocks = (groups + kRotThreads - 1) / kRotThreads;
+    const int64_t blocks = (warps + kRotThreads / 32 - 1) / (kRotThreads / 32);
     const dim3 grid((unsigned)blocks, (unsigned)ceil_div(total, per));
     auto kernel = interleaved ? rotate_kernel<T, VP, NU, true> : rotate_kernel<T, VP, NU, false>;
-    return launch_kernel(kernel, grid, dim3(kRotThreads), 0, stream, a, lp_log, per);
+    return launch_kernel(kernel, grid, dim3(kRotThreads), 0, stream, a, lanes, per);
 }
 
 // Runs of VP elements may be taken together when every address they start at is a multiple of their size.
@@ -339,8 +379,11 @@ extern "C" int octo_patch_positions(int32_t device, const octo_item_t* d_items, 
         return OCTO_E_ALIGNMENT;
     DeviceScope scope(device);
     if (scope.error != cudaSuccess) return report_cuda_error(scope.error, "octo_patch_positions");
-    const cudaError_t e = launch_positions(d_items, max_items, d_n_items, slot_w, slot_h, patch, keep_aspect, d_times,
-                                           n_frames, d_positions, d_visible, static_cast<cudaStream_t>(cuda_stream));
+    int sms = 0;
+    cudaError_t e = sm_count_of(device, &sms);
+    if (e == cudaSuccess)
+        e = launch_positions(d_items, max_items, d_n_items, slot_w, slot_h, patch, keep_aspect, d_times, n_frames, d_positions,
+                             d_visible, sms, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? OCTO_OK : report_cuda_error(e, "octo_patch_positions");
 }
 

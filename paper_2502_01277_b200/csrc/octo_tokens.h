@@ -26,11 +26,19 @@ struct DeviceScope {
 inline bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+// Division by a number that is the same for a whole launch: exact for 0 <= n < 2^31 (multiply by the reciprocal rounded
+// up to 33 bits, whose top bit is the addition of n).
+struct FastDiv {
+    unsigned mul, shift;
+    void set(unsigned d) {
+        shift = 0;
+        while ((1ull << shift) < d) ++shift;
+        mul = (unsigned)(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
+    }
+    __device__ __forceinline__ int div(int n) const { return (int)((__umulhi(mul, (unsigned)n) + (unsigned)n) >> shift); }
+};
+
 // Number of SMs of a device (looked up once per device and process).
 cudaError_t sm_count_of(int device, int* out);
-
-cudaError_t launch_positions(const octo_item_t* d_items, int max_items, const int* d_n_items, int slot_w, int slot_h,
-                             int patch, int keep_aspect, const float* d_times, int n_frames, float* d_positions,
-                             uint8_t* d_visible, cudaStream_t stream);
 
 }  // namespace octo
