@@ -10,19 +10,24 @@
 namespace octo {
 
 // ---------------------------------------------------------------------------------------
-// Few query rows (one new token per item): bound by reading every key and value once.  A CTA takes 16 rows --
-// pairs (query row, head) that share a key head -- of one segment and one split; each of its warps walks over
-// the keys in groups of 16, four warps side by side, with a softmax of its own that the warps join at the end.
-// Keys and values go from global memory straight into the operand registers of the matrix instruction: which
-// element of a head an operand's slot holds is free as long as both operands agree, so the slots are dealt out
-// such that a lane's part of a key is 16 bytes in a row, and a lane's part of the values the same 16 bytes of
-// four keys, paired up by byte permutes.  No shared memory, no barrier before the end; the loads of the next
-// group are in flight while the current one is worked on.
+// Few query rows (one new token per item): bound by reading every key and value once.  A CTA takes the rows -- pairs
+// (query row, head) that share a key head, at most 16 -- of one segment and one split; each of its warps walks
+// over the keys in groups of 16, four warps side by side, with a softmax of its own that the warps join at the end.
+// Keys are the long side of the matrix instruction (16 x 8 x 16) and rows the short one, S^T = K Q^T and O^T = V^T P^T, so
+// that eight rows fill it.  Keys and values go from global memory straight into its operand registers: which element
+// of a head an operand's slot holds is free as long as both operands agree, so the slots are dealt out such
+// that a lane's part of a key is 16 bytes in a row, and a lane's part of the values the same 16 bytes of four
+// keys, paired up by byte permutes.  No shared memory and no barrier before the end; the loads of the next
+// group are in flight while the current one is worked on.  Under a mask the visible keys are listed first, a
+// window at a time, and only those are fetched.
 // ---------------------------------------------------------------------------------------
 constexpr int kStepThreads = 128;
 constexpr int kStepWarps = kStepThreads / 32;
 constexpr int kStepRows = 16;
 constexpr int kStepKeys = 16 * kStepWarps;  // keys a CTA takes per turn
+constexpr int kStepFill = 9;
+constexpr int kStepWindow = 2048;           // keys that are looked through for visible ones at a time
+constexpr float kStepSlack = 8.0f;          // a row's reference follows its maximum when that has grown by 2^8
 
 template <typename T>
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -48,206 +53,226 @@ __device__ __forceinline__ uint4 ldg128(const void* p, bool take) {
     return v;
 }
 
-// DB: 64-element blocks of a head.
-template <typename T, int DB>
-__global__ void __launch_bounds__(kStepThreads)
-attend_step_kernel(const __grid_constant__ AttendArgs a, int row_tiles) {
+// 8 x 8 elements of 16 bits, two in a row per lane: the transposed matrix.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+
+// DB: 64-element blocks of a head.  NT: groups of eight rows.
+template <typename T, int DB, int NT, bool MASKED>
+__global__ void __launch_bounds__(kStepThreads, (DB == 1 ? 2 : 1) * (NT == 1 ? 3 : 2) - (DB == 1 ? 1 : 0))
+attend_step_kernel(const __grid_constant__ AttendArgs a) {
     constexpr int KB = 2 * DB;  // 32-element blocks
-    constexpr int SP = DB * 64 + 4;
-    __shared__ float s_o[kStepWarps][kStepRows][SP];
-    __shared__ float s_m[kStepWarps][kStepRows], s_l[kStepWarps][kStepRows];
+    constexpr int SP = DB * 64 + 4, ROWS = 8 * NT;
+    __shared__ float s_o[kStepWarps][ROWS][SP];
+    __shared__ float s_m[kStepWarps][ROWS], s_l[kStepWarps][ROWS];
+    __shared__ int s_list[MASKED ? kStepWindow : 1], s_seen[kStepWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     unsigned x = blockIdx.x;
     const int split = (int)(x % (unsigned)a.splits);
     x /= (unsigned)a.splits;
-    const int tile = (int)(x % (unsigned)row_tiles);
-    x /= (unsigned)row_tiles;
     const int kvh = (int)(x % (unsigned)a.kv_heads), seg_no = (int)(x / (unsigned)a.kv_heads);
     pdl_wait();
     const Segment seg = segment_of(a, seg_no);
-    const int rows = seg.qn * a.group;
-    if (tile * kStepRows >= rows) return;
+    const int rows = min(seg.qn * a.group, ROWS);
+    if (rows == 0) return;
     const int kb = min(split * a.chunk, seg.kn), ke = min(kb + a.chunk, seg.kn);
     if (split > 0 && kb >= ke) return;
     const int active = a.splits == 1 ? 1 : (seg.kn + a.chunk - 1) / a.chunk;
 
-    // queries: rows g and g + 8 of the tile, 8 elements at 32 b + 8 t of each
-    uint4 qa[KB], qb[KB];
+    // queries: row g of every group, 8 elements at 32 b + 8 t
+    uint4 q[NT][KB];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int vr = tile * kStepRows + g + 8 * half;
-        const int row = vr / a.group, head = kvh * a.group + (vr - row * a.group);
+    for (int n = 0; n < NT; ++n) {
+        const int r = 8 * n + g, row = a.group_div.div(r), head = kvh * a.group + (r - row * a.group);
         const T* p = static_cast<const T*>(a.q) + (seg.q0 + row) * a.q_row + head * a.q_head;
 #pragma unroll
-        for (int b = 0; b < KB; ++b) {
-            const int d = 32 * b + 8 * t;
-            (half ? qb : qa)[b] = ldg128(p + d, vr < rows && d < a.dim);
-        }
+        for (int b = 0; b < KB; ++b) q[n][b] = ldg128(p + 32 * b + 8 * t, r < rows && 32 * b + 8 * t < a.dim);
     }
 
-    const T* const kp = static_cast<const T*>(a.k) + kvh * a.k_head + 8 * t;
-    const T* const vp = static_cast<const T*>(a.v) + kvh * a.v_head + 8 * g;
-    const uint8_t* const mp = a.mask ? a.mask + seg.k0 : nullptr;
-    auto bits_of = [&](int key) -> unsigned {  // one bit per key of the group that counts
-        const int at = key + lane;
-        bool seen = lane < 16 && at < ke;
-        if (seen && mp) seen = mp[at] != 0;
-        return __ballot_sync(0xffffffffu, seen);
-    };
-    uint4 kr[2][KB], vr[4][DB];
-    auto load_k = [&](int key, unsigned bits) {
+    const T* const kp = static_cast<const T*>(a.k) + seg.k0 * a.k_row + kvh * a.k_head + 8 * t;
+    const T* const vp = static_cast<const T*>(a.v) + seg.k0 * a.v_row + kvh * a.v_head + 8 * g;
+    float o[NT][DB * 4][4];
+    float ref[NT][2], sum[NT][2];  // rows 2 t and 2 t + 1 of every group: what the exponents are taken against, sum of weights
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const T* p = kp + (seg.k0 + key + 8 * j + g) * a.k_row;
-            const bool seen = (bits >> (8 * j + g)) & 1u;
+    for (int n = 0; n < NT; ++n) {
+        ref[n][0] = ref[n][1] = -INFINITY;
+        sum[n][0] = sum[n][1] = 0.0f;
 #pragma unroll
-            for (int b = 0; b < KB; ++b) kr[j][b] = ldg128(p + 32 * b, seen && 32 * b + 8 * t < a.dim);
-        }
-    };
-    auto load_v = [&](int key, unsigned bits) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int n = 2 * t + (j & 1) + 8 * (j >> 1);
-            const T* p = vp + (seg.k0 + key + n) * a.v_row;
-            const bool seen = (bits >> n) & 1u;
-#pragma unroll
-            for (int b = 0; b < DB; ++b) vr[j][b] = ldg128(p + 64 * b, seen && 64 * b + 8 * g < a.dim);
-        }
-    };
-
-    float o[DB * 8][4];
-#pragma unroll
-    for (int i = 0; i < DB * 8; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;  // rows g and g + 8
-
-    int key = kb + 16 * warp;
-    unsigned bits = bits_of(key);
-    load_k(key, bits);
-    load_v(key, bits);
-    unsigned next = bits_of(key + kStepKeys);
-    for (; key < ke; key += kStepKeys) {
-        const unsigned after = bits_of(key + 2 * kStepKeys);
-        if (bits == 0) {  // nothing to see: only fetch the next group
-            load_k(key + kStepKeys, next);
-            load_v(key + kStepKeys, next);
-            bits = next;
-            next = after;
-            continue;
-        }
-        float s[2][4];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.0f;
-#pragma unroll
-            for (int b = 0; b < KB; ++b) {
-                mma_16816<T>(s[j], qa[b].x, qb[b].x, qa[b].y, qb[b].y, kr[j][b].x, kr[j][b].y);
-                mma_16816<T>(s[j], qa[b].z, qb[b].z, qa[b].w, qb[b].w, kr[j][b].z, kr[j][b].w);
-            }
-        }
-        load_k(key + kStepKeys, next);
-        // scores of this lane: keys 8 j + 2 t and + 1, rows g (0, 1) and g + 8 (2, 3)
-        float t0 = -INFINITY, t1 = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[j][i] = (bits >> (8 * j + 2 * t + (i & 1))) & 1u ? s[j][i] * a.scale_log2 : -INFINITY;
-                if (i < 2) t0 = fmaxf(t0, s[j][i]);
-                else t1 = fmaxf(t1, s[j][i]);
-            }
-        t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, 1));
-        t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, 1));
-        t0 = fmaxf(m0, fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, 2)));
-        t1 = fmaxf(m1, fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, 2)));
-        const float r0 = t0 == -INFINITY ? 0.0f : t0, r1 = t1 == -INFINITY ? 0.0f : t1;
-        if (__any_sync(0xffffffffu, t0 != m0 || t1 != m1)) {  // a larger maximum: what was summed shrinks
-            const float f0 = ex2(m0 - r0), f1 = ex2(m1 - r1);
-            l0 *= f0;
-            l1 *= f1;
-#pragma unroll
-            for (int i = 0; i < DB * 8; ++i) {
-                o[i][0] *= f0;
-                o[i][1] *= f0;
-                o[i][2] *= f1;
-                o[i][3] *= f1;
-            }
-            m0 = t0;
-            m1 = t1;
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            s[j][0] = ex2(s[j][0] - r0);
-            s[j][1] = ex2(s[j][1] - r0);
-            s[j][2] = ex2(s[j][2] - r1);
-            s[j][3] = ex2(s[j][3] - r1);
-            l0 += s[j][0] + s[j][1];
-            l1 += s[j][2] + s[j][3];
-        }
-        // the weights in the type of the values: what the matrix instruction takes (the sum keeps them unrounded)
-        const uint32_t p0 = pack2<T>(s[0][0], s[0][1]), p1 = pack2<T>(s[0][2], s[0][3]);
-        const uint32_t p2 = pack2<T>(s[1][0], s[1][1]), p3 = pack2<T>(s[1][2], s[1][3]);
-#pragma unroll
-        for (int b = 0; b < DB; ++b) {
-            const uint32_t* v0 = reinterpret_cast<const uint32_t*>(&vr[0][b]);
-            const uint32_t* v1 = reinterpret_cast<const uint32_t*>(&vr[1][b]);
-            const uint32_t* v2 = reinterpret_cast<const uint32_t*>(&vr[2][b]);
-            const uint32_t* v3 = reinterpret_cast<const uint32_t*>(&vr[3][b]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const unsigned pick = i & 1 ? 0x7632u : 0x5410u;
-                mma_16816<T>(o[8 * b + i], p0, p1, p2, p3, __byte_perm(v0[i / 2], v1[i / 2], pick),
-                             __byte_perm(v2[i / 2], v3[i / 2], pick));
-            }
-        }
-        load_v(key + kStepKeys, next);
-        bits = next;
-        next = after;
+        for (int i = 0; i < DB * 4; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
     }
 
-    // join the warps: o[8 b + i] of this lane are elements 64 b + 16 t + i (0, 2) and + 8 (1, 3) of rows g and g + 8
-    l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
-    l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
-    l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
-    l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
-    if (t == 0) {
-        s_m[warp][g] = m0;
-        s_l[warp][g] = l0;
-        s_m[warp][g + 8] = m1;
-        s_l[warp][g + 8] = l1;
-    }
+    for (int wb = kb; wb < ke; wb += kStepWindow) {
+        int count = ke - wb;
+        if (MASKED) {
+            // the visible keys of the window, every warp's one after the other
+            const uint8_t* const mask = a.mask + seg.k0 + wb;
+            unsigned bits = 0;
+            int mine = 0;
+            const int limit = min(count, kStepWindow);
 #pragma unroll
-    for (int b = 0; b < DB; ++b)
-#pragma unroll
-        for (int i = 0; i < 8; i += 4)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                float4 f = make_float4(o[8 * b + i][c], o[8 * b + i + 1][c], o[8 * b + i + 2][c], o[8 * b + i + 3][c]);
-                *reinterpret_cast<float4*>(&s_o[warp][g + 8 * (c >> 1)][64 * b + 16 * t + 8 * (c & 1) + i]) = f;
+            for (int j = 0; j < kStepWindow / kStepThreads; ++j) {
+                const int at = j * kStepThreads + (int)threadIdx.x;
+                if (at < limit && mask[at] != 0) bits |= 1u << j;
             }
+#pragma unroll
+            for (int j = 0; j < kStepWindow / kStepThreads; ++j) mine += __popc(__ballot_sync(0xffffffffu, (bits >> j) & 1u));
+            __syncthreads();  // (the list of the window before has been read)
+            if (lane == 0) s_seen[warp] = mine;
+            __syncthreads();
+            int at = 0;
+            count = 0;
+#pragma unroll
+            for (int w = 0; w < kStepWarps; ++w) {
+                if (w < warp) at += s_seen[w];
+                count += s_seen[w];
+            }
+#pragma unroll
+            for (int j = 0; j < kStepWindow / kStepThreads; ++j) {
+                const bool seen = (bits >> j) & 1u;
+                const unsigned ballot = __ballot_sync(0xffffffffu, seen);
+                if (seen) s_list[at + __popc(ballot & ((1u << lane) - 1u))] = j * kStepThreads + (int)threadIdx.x;
+                at += __popc(ballot);
+            }
+            __syncthreads();
+        }
+        auto key_at = [&](int n) -> int64_t { return wb + (MASKED ? s_list[n] : n); };
+        uint4 kr[2][KB], vr[4][DB];
+        auto load_k = [&](int first) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int n = first + 8 * j + g;
+                const bool there = n < count;
+                const T* p = kp + (there ? key_at(n) : 0) * a.k_row;
+#pragma unroll
+                for (int b = 0; b < KB; ++b) kr[j][b] = ldg128(p + 32 * b, there && 32 * b + 8 * t < a.dim);
+            }
+        };
+        auto load_v = [&](int first) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int n = first + 2 * t + (j & 1) + 8 * (j >> 1);
+                const bool there = n < count;
+                const T* p = vp + (there ? key_at(n) : 0) * a.v_row;
+#pragma unroll
+                for (int b = 0; b < DB; ++b) vr[j][b] = ldg128(p + 64 * b, there && 64 * b + 8 * g < a.dim);
+            }
+        };
+        int first = 16 * warp;
+        load_k(first);
+        load_v(first);
+        for (; first < count; first += kStepKeys) {
+            float s[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+#pragma unroll
+                for (int b = 0; b < KB; ++b) {
+                    mma_16816<T>(s[n], kr[0][b].x, kr[1][b].x, kr[0][b].y, kr[1][b].y, q[n][b].x, q[n][b].y);
+                    mma_16816<T>(s[n], kr[0][b].z, kr[1][b].z, kr[0][b].w, kr[1][b].w, q[n][b].z, q[n][b].w);
+                }
+            }
+            load_k(first + kStepKeys);
+            // this lane's scores: keys g (0, 1) and g + 8 (2, 3), rows 2 t (0, 2) and 2 t + 1 (1, 3)
+            const bool in0 = first + g < count, in1 = first + g + 8 < count;
+            bool grown = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[n][i] = (i < 2 ? in0 : in1) ? s[n][i] * a.scale_log2 : -INFINITY;
+                    grown = grown || s[n][i] > ref[n][i & 1] + kStepSlack || (ref[n][i & 1] == -INFINITY && s[n][i] > -INFINITY);
+                }
+            if (__any_sync(0xffffffffu, grown)) {  // (not for NaN, which comes through the weights)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float top = fmaxf(s[n][c], s[n][c + 2]);
+#pragma unroll
+                        for (int m = 4; m < 32; m <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+                        top = fmaxf(top, ref[n][c]);
+                        const float f = top == -INFINITY ? 1.0f : ex2(ref[n][c] - top);  // what was summed shrinks
+                        ref[n][c] = top;
+                        sum[n][c] *= f;
+#pragma unroll
+                        for (int i = 0; i < DB * 4; ++i) {
+                            o[n][i][c] *= f;
+                            o[n][i][c + 2] *= f;
+                        }
+                    }
+            }
+            uint32_t p0[NT], p1[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[n][i] = ex2(s[n][i] - (ref[n][i & 1] == -INFINITY ? 0.0f : ref[n][i & 1]));
+                sum[n][0] += s[n][0] + s[n][2];
+                sum[n][1] += s[n][1] + s[n][3];
+                // the weights in the type of the values: what the matrix instruction takes (the sum keeps them unrounded)
+                p0[n] = transpose8x8(pack2<T>(s[n][0], s[n][1]));
+                p1[n] = transpose8x8(pack2<T>(s[n][2], s[n][3]));
+            }
+#pragma unroll
+            for (int b = 0; b < DB; ++b) {
+                const uint32_t* v0 = reinterpret_cast<const uint32_t*>(&vr[0][b]);
+                const uint32_t* v1 = reinterpret_cast<const uint32_t*>(&vr[1][b]);
+                const uint32_t* v2 = reinterpret_cast<const uint32_t*>(&vr[2][b]);
+                const uint32_t* v3 = reinterpret_cast<const uint32_t*>(&vr[3][b]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {  // elements 64 b + 8 g + 2 i and + 1 of this lane's piece
+                    const uint32_t a0 = __byte_perm(v0[i], v1[i], 0x5410), a1 = __byte_perm(v0[i], v1[i], 0x7632);
+                    const uint32_t a2 = __byte_perm(v2[i], v3[i], 0x5410), a3 = __byte_perm(v2[i], v3[i], 0x7632);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) mma_16816<T>(o[n][4 * b + i], a0, a1, a2, a3, p0[n], p1[n]);
+                }
+            }
+            load_v(first + kStepKeys);
+        }
+        if (!MASKED) break;
+    }
+
+    // join the warps: o[n][4 b + i] of this lane are elements 64 b + 8 g + 2 i (0, 1) and + 1 (2, 3) of rows 2 t (0, 2), 2 t + 1 (1, 3)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+            for (int m = 4; m < 32; m <<= 1) sum[n][c] += __shfl_xor_sync(0xffffffffu, sum[n][c], m);
+            const int r = 8 * n + 2 * t + c;
+            if (g == 0) {
+                s_m[warp][r] = ref[n][c];
+                s_l[warp][r] = sum[n][c];
+            }
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; i += 2)
+                    *reinterpret_cast<float4*>(&s_o[warp][r][64 * b + 8 * g + 2 * i]) =
+                        make_float4(o[n][4 * b + i][c], o[n][4 * b + i][c + 2], o[n][4 * b + i + 1][c], o[n][4 * b + i + 1][c + 2]);
+        }
     __syncthreads();
-    const int r = threadIdx.x >> 3, vrow = tile * kStepRows + r;
-    if (vrow >= rows) return;
+    constexpr int PER = kStepThreads / ROWS;  // threads of a row, 8 elements of it at a time
+    const int r = threadIdx.x / PER, part_of = threadIdx.x % PER;
+    if (r >= rows) return;
     float top = s_m[0][r];
 #pragma unroll
     for (int w = 1; w < kStepWarps; ++w) top = fmaxf(top, s_m[w][r]);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float share[kStepWarps], sum = 0.0f;
+    const float base = top == -INFINITY ? 0.0f : top;
+    float share[kStepWarps], total = 0.0f;
 #pragma unroll
     for (int w = 0; w < kStepWarps; ++w) {
-        share[w] = ex2(s_m[w][r] - ref);
-        sum += share[w] * s_l[w][r];
+        share[w] = ex2(s_m[w][r] - base);
+        total += share[w] * s_l[w][r];
     }
-    const int row = vrow / a.group, head = kvh * a.group + (vrow - row * a.group);
+    const int row = a.group_div.div(r), head = kvh * a.group + (r - row * a.group);
     const int64_t part = ((int64_t)split * a.q_total + seg.q0 + row) * a.heads + head;
     const bool last = active <= 1;
-    const float inv = last ? (sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f) : 1.0f;
-    T* out = static_cast<T*>(a.out) + (seg.q0 + row) * a.o_row + head * a.o_head;
-#pragma unroll
-    for (int b = 0; b < DB; ++b) {
-        const int d = 64 * b + 8 * (threadIdx.x & 7);
-        if (d >= a.dim) continue;
+    const float inv = last ? (total > 0.0f || total != total ? 1.0f / total : 0.0f) : 1.0f;
+    T* const out = static_cast<T*>(a.out) + (seg.q0 + row) * a.o_row + head * a.o_head;
+    for (int d = 8 * part_of; d < a.dim; d += 8 * PER) {
         float f[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -269,7 +294,7 @@ attend_step_kernel(const __grid_constant__ AttendArgs a, int row_tiles) {
             p[1] = make_float4(f[4], f[5], f[6], f[7]);
         }
     }
-    if (!last && (threadIdx.x & 7) == 0) a.part_ml[part] = make_float2(top, sum);
+    if (!last && part_of == 0) a.part_ml[part] = make_float2(top, total);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -380,11 +405,14 @@ static int make_plan(const octo_attend_t* c, int sms, AttendPlan* p) {
     // no more tiles than the rows make, with one that is not full in every segment
     const int64_t rows_make = (c->q_total * group + tile_rows - 1) / tile_rows + c->segments;
     const int64_t busy = units < rows_make * c->kv_heads ? units : rows_make * c->kv_heads;
-    const int64_t want = p->tile ? sms : (int64_t)sms * 12;
-    int64_t splits = p->tile ? (want / busy < 1 ? 1 : want / busy) : (busy >= want ? 1 : (want + busy - 1) / busy);
-    int64_t chunk = (max_k + splits - 1) / splits;
-    if (chunk < 512) chunk = 512;
-    chunk = (chunk + step - 1) / step * step;
+    // Work is split over the keys while that keeps more of the GPU busy: tiles up to one per SM, few rows up to
+    // kStepFill CTAs per SM; a split has 512 keys at least, and all are of one size.
+    const int64_t want = p->tile ? sms : (int64_t)sms * kStepFill;
+    int64_t splits = p->tile ? want / busy : (want + busy - 1) / busy;
+    const int64_t most = (max_k + 511) / 512;
+    if (splits > most) splits = most;
+    if (splits < 1) splits = 1;
+    const int64_t chunk = ((max_k + splits - 1) / splits + step - 1) / step * step;
     splits = (max_k + chunk - 1) / chunk;
     p->splits = (int)splits;
     p->chunk = splits == 1 ? (int)max_k : (int)chunk;
@@ -400,8 +428,15 @@ static cudaError_t launch_attend(const AttendArgs& a, const AttendPlan& p, cudaS
     if (p.tile) {
         e = launch_attend_tile(a, std::is_same<T, __nv_bfloat16>::value, (int)p.ctas, (int)p.row_tiles, stream);
     } else {
-        auto kernel = a.dim <= 64 ? attend_step_kernel<T, 1> : attend_step_kernel<T, 2>;
-        e = launch_kernel(kernel, dim3((unsigned)p.ctas), dim3(kStepThreads), 0, stream, a, (int)p.row_tiles);
+        const bool eight = a.max_q * a.group <= 8;
+        void (*kernel)(const AttendArgs);
+        if (a.dim <= 64)
+            kernel = a.mask ? (eight ? attend_step_kernel<T, 1, 1, true> : attend_step_kernel<T, 1, 2, true>)
+                            : (eight ? attend_step_kernel<T, 1, 1, false> : attend_step_kernel<T, 1, 2, false>);
+        else
+            kernel = a.mask ? (eight ? attend_step_kernel<T, 2, 1, true> : attend_step_kernel<T, 2, 2, true>)
+                            : (eight ? attend_step_kernel<T, 2, 1, false> : attend_step_kernel<T, 2, 2, false>);
+        e = launch_kernel(kernel, dim3((unsigned)p.ctas), dim3(kStepThreads), 0, stream, a);
     }
     if (e == cudaSuccess && a.splits > 1) {
         const int64_t blocks = (a.q_total * a.heads * 32 + kJoinThreads - 1) / kJoinThreads;
