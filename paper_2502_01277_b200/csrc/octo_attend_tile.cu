@@ -200,7 +200,9 @@ __device__ __forceinline__ void tile_row(const AttendArgs& a, int kvh, int r, in
 
 // One wait of a role.  A wait that runs out is reported; the role then leaves, and so do the others in turn.
 __device__ __forceinline__ bool tile_wait(uint64_t* bar, uint32_t parity, unsigned int* status) {
-    if (mbar_wait_bounded(bar, parity)) return true;
+#pragma unroll 1  // (the loops of five roles were a third of the kernel's code)
+    for (int i = 0; i < 1 << 20; ++i)
+        if (mbar_try_wait(bar, parity)) return true;
     if (status) atomicOr(status, OCTO_STATUS_COPY_TIMEOUT);
     return false;
 }
@@ -233,6 +235,7 @@ struct Loader {
     }
     __device__ __forceinline__ void flush() {
         asm volatile("cp.async.wait_group 0;" ::: "memory");
+#pragma unroll 1
         while (in_flight > 0) arrive_oldest();
     }
     // Whoever waits hands over what has landed first: the wait may be for a consumer of just that.
@@ -293,7 +296,7 @@ struct Loader {
     // The queries' tile; at(r) gives a row's address, or null for zeros.
     template <typename F>
     __device__ __forceinline__ void queries(uint32_t dst, F at) {
-#pragma unroll 8
+#pragma unroll 4
         for (int j = 0; j < kOwn; ++j) {
             const char* p = at(row(j));
             const bool take = wide && p != nullptr;
@@ -462,6 +465,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                         if (!first) {  // (of the products, all but the last turn's are complete: the scores came after them)
                             if (!__all_sync(0xffffffffu, tile_wait(&sh->pv_done[h][(turn - 1) & 1], ((turn - 1) >> 1) & 1, a.status))) dead = true;
                             tmem_after_sync();
+#pragma unroll 1
                             for (int c = 0; c < o_chunks; ++c) {
                                 tmem_ld32(o_at + 32 * c, p);
                                 tmem_landed(p);
@@ -514,6 +518,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                     real[k] = r < end;
                     row_out[k] = static_cast<T*>(a.out) + (it.q0 + qrow) * a.o_row + head * a.o_head + 8 * (lane & 3);
                 }
+#pragma unroll 1
                 for (int c = 0; c < o_chunks; ++c) {
                     uint32_t o[32];
                     tmem_ld32(o_at + 32 * c, o);
@@ -541,6 +546,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                 int qrow, head;
                 tile_row(a, it.kvh, r, qrow, head);
                 const int64_t at = ((int64_t)it.split * a.q_total + it.q0 + qrow) * a.heads + head;
+#pragma unroll 1
                 for (int c = 0; c < o_chunks; ++c) {
                     uint32_t o[32];
                     __syncwarp();
@@ -559,6 +565,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
         }
         if (dead) {  // a wait has run out: rows that are not done say so
             const float nan = __int_as_float(0x7fffffff);
+#pragma unroll 1
             for (int64_t w = done_work < 0 ? blockIdx.x : done_work + gridDim.x; w < total; w += gridDim.x) {
                 TileItem it;
                 if (!tile_item(a, prefix, tiles_per_segment, w, it)) continue;
@@ -569,6 +576,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                 T* const out = static_cast<T*>(a.out) + (it.seg.q0 + qrow) * a.o_row + head * a.o_head;
                 const int64_t at = ((int64_t)it.split * a.q_total + it.seg.q0 + qrow) * a.heads + head;
                 if (!it.last) a.part_ml[at] = make_float2(0.0f, nan);
+#pragma unroll 1
                 for (int d = 0; it.last && d < a.dim; d += 2) *reinterpret_cast<uint32_t*>(out + d) = pack2<T>(nan, nan);
             }
         }
@@ -787,7 +795,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                         last = cursor >= it.ke;
                     }
                     if (warp == 10 && lane == 0) sh->meta[tile & 15] = take | (last ? 1 << 16 : 0);
-#pragma unroll
+#pragma unroll 1
                     for (int which = 0; which < 2; ++which) {
                         const uint32_t n = ld.slot;
                         ld.wait(&sh->empty[n % Shape::kStages], ((n / Shape::kStages) & 1) ^ 1);
