@@ -563,7 +563,7 @@ typedef struct {
     int64_t max_q, max_k;             /* most query / key rows of a segment; rows of a longer segment from */
                                       /* there on are left / not looked at.  0: not known                  */
     const uint8_t* d_key_mask;        /* [k_total] or NULL                                                 */
-    float scale;                      /* finite                                                            */
+    float scale;                      /* magnitude at most 1e30                                            */
     float _pad;
     uint32_t* d_status;               /* one word, or NULL: OCTO_STATUS_COPY_TIMEOUT is set (and the rows  */
                                       /* concerned become NaN) if a bounded wait of the kernel gives up    */

@@ -89,7 +89,9 @@ attend_step_kernel(const __grid_constant__ AttendArgs a) {
         const int r = 8 * n + g, row = a.group_div.div(r), head = kvh * a.group + (r - row * a.group);
         const T* p = static_cast<const T*>(a.q) + (seg.q0 + row) * a.q_row + head * a.q_head;
 #pragma unroll
-        for (int b = 0; b < KB; ++b) q[n][b] = ldg128(p + 32 * b + 8 * t, r < rows && 32 * b + 8 * t < a.dim);
+        for (int b = 0; b < KB; ++b)
+            q[n][b] = ldg128(p + 32 * b + 8 * t, r < rows && 32 * b + 8 * t < a.dim &&
+                                                     OCTO_TOKEN_IN_RANGE(seg.q0 + row < a.q_total && head < a.heads, a.status));
     }
 
     const T* const kp = static_cast<const T*>(a.k) + seg.k0 * a.k_row + kvh * a.k_head + 8 * t;
@@ -139,12 +141,13 @@ attend_step_kernel(const __grid_constant__ AttendArgs a) {
             __syncthreads();
         }
         auto key_at = [&](int n) -> int64_t { return wb + (MASKED ? s_list[n] : n); };
+        auto in_keys = [&](int n) { return n >= 0 && (!MASKED || n < kStepWindow) && key_at(n) < ke && seg.k0 + key_at(n) < a.k_total; };
         uint4 kr[2][KB], vr[4][DB];
         auto load_k = [&](int first) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int n = first + 8 * j + g;
-                const bool there = n < count;
+                const bool there = n < count && OCTO_TOKEN_IN_RANGE(in_keys(n), a.status);
                 const T* p = kp + (there ? key_at(n) : 0) * a.k_row;
 #pragma unroll
                 for (int b = 0; b < KB; ++b) kr[j][b] = ldg128(p + 32 * b, there && 32 * b + 8 * t < a.dim);
@@ -154,7 +157,7 @@ attend_step_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int n = first + 2 * t + (j & 1) + 8 * (j >> 1);
-                const bool there = n < count;
+                const bool there = n < count && OCTO_TOKEN_IN_RANGE(in_keys(n), a.status);
                 const T* p = vp + (there ? key_at(n) : 0) * a.v_row;
 #pragma unroll
                 for (int b = 0; b < DB; ++b) vr[j][b] = ldg128(p + 64 * b, there && 64 * b + 8 * g < a.dim);
@@ -256,7 +259,7 @@ attend_step_kernel(const __grid_constant__ AttendArgs a) {
     __syncthreads();
     constexpr int PER = kStepThreads / ROWS;  // threads of a row, 8 elements of it at a time
     const int r = threadIdx.x / PER, part_of = threadIdx.x % PER;
-    if (r >= rows) return;
+    if (r >= rows || !OCTO_TOKEN_IN_RANGE(seg.q0 + a.group_div.div(r) < a.q_total, a.status)) return;
     float top = s_m[0][r];
 #pragma unroll
     for (int w = 1; w < kStepWarps; ++w) top = fmaxf(top, s_m[w][r]);
@@ -382,7 +385,7 @@ static int validate(const octo_attend_t* c) {
     if (c->q_rows < 1 || c->k_rows < 1 || c->q_rows > most || c->k_rows > most) return OCTO_E_INVALID_ARG;
     if (c->q_first < -most || c->q_first > most || c->k_first < -most || c->k_first > most) return OCTO_E_INVALID_ARG;
     if (c->max_q < 0 || c->max_k < 0) return OCTO_E_INVALID_ARG;
-    if (!(fabsf(c->scale) <= 3e38f)) return OCTO_E_INVALID_ARG;
+    if (!(fabsf(c->scale) <= 1e30f)) return OCTO_E_INVALID_ARG;
     if ((c->d_q_offsets || c->d_k_offsets) && c->segments > OCTO_MAX_SEGMENTS) return OCTO_E_CAPACITY;
     return OCTO_OK;
 }

@@ -8,6 +8,17 @@
 
 namespace octo {
 
+// Range checks of the checked build for kernels whose status word may be missing (see OCTO_IN_RANGE).
+#ifdef OCTO_BOUNDS_CHECK
+__device__ __forceinline__ bool token_in_range(bool ok, unsigned int* status) {
+    if (!ok && status) atomicOr(status, OCTO_STATUS_BOUNDS);
+    return ok;
+}
+#define OCTO_TOKEN_IN_RANGE(cond, status_ptr) token_in_range((cond), (status_ptr))
+#else
+#define OCTO_TOKEN_IN_RANGE(cond, status_ptr) (true)
+#endif
+
 struct AttendArgs {
     const void *q, *k, *v;
     void* out;

@@ -274,7 +274,7 @@ struct Loader {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int g = warp + kLoadWarps * ((b + i) / kTurns), r = row(b + i);
-                const bool take_it = wide && r < take;
+                const bool take_it = wide && r < take && OCTO_TOKEN_IN_RANGE(key(r) >= 0 && key(r) < end, status);
                 const char* const p = take_it ? src + (int64_t)key(r) * stride : zero_row;
                 if (g < groups) cp_async16(dst + (uint32_t)g * 1024u + place[i % kTurns], p, take_it);
             }
@@ -304,6 +304,7 @@ struct Loader {
         }
     }
     const char* zero_row;  // any valid address
+    int end;               // key rows of the segment
 };
 
 template <typename T, int DB>
@@ -496,7 +497,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
             }
             if (dead || (meta & kStop)) break;
             // the half's rows of the result
-            const TileInfo it = sh->info[meta >> kItemShift];
+            const TileInfo it = sh->info[OCTO_TOKEN_IN_RANGE((unsigned)(meta >> kItemShift) < 4u, a.status) ? meta >> kItemShift : 0];
             if (!__all_sync(0xffffffffu, tile_wait(&sh->pv_done[h][(turn - 1) & 1], ((turn - 1) >> 1) & 1, a.status))) {
                 dead = true;
                 break;
@@ -515,7 +516,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                     const int r = r0 + (row & ~31) + 8 * k + (lane >> 2);
                     int qrow, head;
                     tile_row(a, it.kvh, r, qrow, head);
-                    real[k] = r < end;
+                    real[k] = r < end && OCTO_TOKEN_IN_RANGE(it.q0 >= 0 && it.q0 + qrow < a.q_total && head < a.heads, a.status);
                     row_out[k] = static_cast<T*>(a.out) + (it.q0 + qrow) * a.o_row + head * a.o_head + 8 * (lane & 3);
                 }
 #pragma unroll 1
@@ -743,6 +744,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                         ld.queries(q_base + (b / kHalf) * Shape::kStageBytes, [&](int r) -> const char* {
                             int qrow, hd;
                             tile_row(a, 0, it.row0 + b + r, qrow, hd);
+                            if (!OCTO_TOKEN_IN_RANGE(b + r >= it.rows || (it.seg.q0 + qrow < a.q_total && hd < a.group), a.status)) return nullptr;
                             return b + r < it.rows ? q + (int64_t)qrow * row + (int64_t)hd * head : nullptr;
                         });
                     if (warp == 10 && lane == 0) {
@@ -759,6 +761,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                     ++items;
                 };
                 bool queries = false;
+                ld.end = OCTO_TOKEN_IN_RANGE(it.seg.k0 >= 0 && it.seg.k0 + it.ke <= a.k_total && it.kvh < a.kv_heads, a.status) ? it.ke : 0;
                 const char* const k = reinterpret_cast<const char*>(static_cast<const T*>(a.k) + it.seg.k0 * a.k_row + it.kvh * a.k_head);
                 const char* const v = reinterpret_cast<const char*>(static_cast<const T*>(a.v) + it.seg.k0 * a.v_row + it.kvh * a.v_head);
                 const uint8_t* const mask = a.mask ? a.mask + it.seg.k0 : nullptr;
@@ -804,7 +807,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                         const int stride = (int)(2 * (which ? a.v_row : a.k_row));
                         const uint32_t dst = ring + (n % Shape::kStages) * Shape::kStageBytes;
                         if (mask) ld.tile(dst, take, src, stride, [&](int r) { return list[r]; });
-                        else if (take == kHalf) ld.full_tile(dst, src + (int64_t)from * stride, stride);
+                        else if (take == kHalf && OCTO_TOKEN_IN_RANGE(from >= 0 && from + kHalf <= it.ke, a.status)) ld.full_tile(dst, src + (int64_t)from * stride, stride);
                         else ld.tile(dst, take, src, stride, [&](int r) { return from + r; });
                         ld.issued(&sh->full[n % Shape::kStages]);
                         ++ld.slot;

@@ -186,3 +186,21 @@ def test_passes_of_64_rows(checked):
 def test_few_columns_of_a_16384_pixel_frame(checked, keep_aspect, oh):
     from test_gpu_crop_tiles import test_few_columns_of_a_16384_pixel_frame as run
     run(keep_aspect, oh)
+
+
+@pytest.mark.parametrize("seed", range(0, 24, 3))
+def test_attention_under_the_checked_build(checked, seed):
+    """(The comparison requires a status word without any bit.)"""
+    from test_gpu_tokens import test_attention_random_calls as run
+    run(seed)
+
+
+@pytest.mark.parametrize("n,q_rows,k_rows,heads,kv", [(1, 1, 20000, 8, 1), (2, 2, 9001, 8, 8), (1, 100, 30000, 2, 1)])
+def test_long_attention_under_the_checked_build(checked, n, q_rows, k_rows, heads, kv):
+    from test_gpu_tokens import BF16, test_attention_long as run
+    run(BF16, n, q_rows, k_rows, heads, kv)
+
+
+def test_crops_attend_to_their_frames_under_the_checked_build(checked):
+    from test_gpu_tokens import test_crops_attend_to_their_frames as run
+    run()
