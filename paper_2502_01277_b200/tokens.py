@@ -49,8 +49,9 @@ def _stream_of(device, stream) -> int:
 
 def _on_device(where, device, *tensors) -> None:
     """Every tensor given lies on `device`: a pointer of another one would be read there."""
+    index = device.index
     for t in tensors:
-        if t is not None and t.device != device:
+        if t is not None and t.get_device() != index:
             _refuse(where, f"a tensor is on {t.device}, not on {device}")
 
 
