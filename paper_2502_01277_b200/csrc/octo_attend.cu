@@ -63,7 +63,7 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
 // DB: 64-element blocks of a head.  NT: groups of eight rows.
 template <typename T, int DB, int NT, bool MASKED>
 __global__ void __launch_bounds__(kStepThreads, (DB == 1 ? 2 : 1) * (NT == 1 ? 3 : 2) - (DB == 1 ? 1 : 0))
-attend_step_kernel(const __grid_constant__ AttendArgs a) {
+attend_step_kernel(const __grid_constant__ AttendArgs a, int row_tiles) {
     constexpr int KB = 2 * DB;  // 32-element blocks
     constexpr int SP = DB * 64 + 4, ROWS = 8 * NT;
     __shared__ float s_o[kStepWarps][ROWS][SP];
@@ -73,11 +73,13 @@ attend_step_kernel(const __grid_constant__ AttendArgs a) {
     unsigned x = blockIdx.x;
     const int split = (int)(x % (unsigned)a.splits);
     x /= (unsigned)a.splits;
+    const int row0 = (int)(x % (unsigned)row_tiles) * ROWS;
+    x /= (unsigned)row_tiles;
     const int kvh = (int)(x % (unsigned)a.kv_heads), seg_no = (int)(x / (unsigned)a.kv_heads);
     pdl_wait();
     const Segment seg = segment_of(a, seg_no);
-    const int rows = min(seg.qn * a.group, ROWS);
-    if (rows == 0) return;
+    const int rows = min(seg.qn * a.group - row0, ROWS);
+    if (rows <= 0) return;
     const int kb = min(split * a.chunk, seg.kn), ke = min(kb + a.chunk, seg.kn);
     if (split > 0 && kb >= ke) return;
     const int active = a.splits == 1 ? 1 : (seg.kn + a.chunk - 1) / a.chunk;
@@ -86,7 +88,7 @@ attend_step_kernel(const __grid_constant__ AttendArgs a) {
     uint4 q[NT][KB];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int r = 8 * n + g, row = a.group_div.div(r), head = kvh * a.group + (r - row * a.group);
+        const int r = 8 * n + g, row = a.group_div.div(row0 + r), head = kvh * a.group + (row0 + r - row * a.group);
         const T* p = static_cast<const T*>(a.q) + (seg.q0 + row) * a.q_row + head * a.q_head;
 #pragma unroll
         for (int b = 0; b < KB; ++b)
@@ -259,7 +261,7 @@ attend_step_kernel(const __grid_constant__ AttendArgs a) {
     __syncthreads();
     constexpr int PER = kStepThreads / ROWS;  // threads of a row, 8 elements of it at a time
     const int r = threadIdx.x / PER, part_of = threadIdx.x % PER;
-    if (r >= rows || !OCTO_TOKEN_IN_RANGE(seg.q0 + a.group_div.div(r) < a.q_total, a.status)) return;
+    if (r >= rows || !OCTO_TOKEN_IN_RANGE(seg.q0 + a.group_div.div(row0 + r) < a.q_total, a.status)) return;
     float top = s_m[0][r];
 #pragma unroll
     for (int w = 1; w < kStepWarps; ++w) top = fmaxf(top, s_m[w][r]);
@@ -270,7 +272,7 @@ attend_step_kernel(const __grid_constant__ AttendArgs a) {
         share[w] = ex2(s_m[w][r] - base);
         total += share[w] * s_l[w][r];
     }
-    const int row = a.group_div.div(r), head = kvh * a.group + (r - row * a.group);
+    const int row = a.group_div.div(row0 + r), head = kvh * a.group + (row0 + r - row * a.group);
     const int64_t part = ((int64_t)split * a.q_total + seg.q0 + row) * a.heads + head;
     const bool last = active <= 1;
     const float inv = last ? (total > 0.0f || total != total ? 1.0f / total : 0.0f) : 1.0f;
@@ -400,7 +402,15 @@ static int make_plan(const octo_attend_t* c, int sms, AttendPlan* p) {
     const int64_t group = c->heads / c->kv_heads;
     const int64_t max_q = bound_of(c->max_q, c->d_q_offsets, c->q_rows, c->q_total);
     const int64_t max_k = bound_of(c->max_k, c->d_k_offsets, c->k_rows, c->k_total);
-    p->tile = max_q * group > kStepRows;
+    // Up to 16 rows a segment the step kernel reads every key once and is always ahead.  More rows take several of its
+    // CTAs, which read the keys again, but a CTA is through in 3 us where a tile takes 7 to 9: it stays ahead while the
+    // whole call is small.  Work in key rows read, with what a CTA costs beside them (256); us tile / step:
+    // 4 segments of 64 rows, 8 key heads of 128, 512 keys 14.1 / 10.0, 2048 keys 18.4 / 26.4; 64 segments of 32 rows, 128
+    // keys 22.9 / 21.5, 512 keys 43 / 54; 64 of 64 rows, 8 key heads of 64, 128 keys 20.9 / 20.7; 8 of 128 rows, 2 key heads,
+    // 512 keys 12.9 / 8.3.
+    const double step_ctas = (double)c->segments * c->kv_heads * (double)((max_q * group + kStepRows - 1) / kStepRows);
+    const double work = step_ctas * (double)(max_k + 256) * (c->head_dim > 64 ? 2 : 1);
+    p->tile = max_q * group > kStepRows && work > (step_ctas >= 4.0 * sms ? 800e3 : 300e3);
     const int64_t tile_rows = p->tile ? kTileRows : kStepRows, step = p->tile ? kTileKeys : kStepKeys;
     p->row_tiles = (max_q * group + tile_rows - 1) / tile_rows;
     if ((double)c->segments * c->kv_heads * (double)p->row_tiles > (double)INT64_MAX / 1024) return OCTO_E_CAPACITY;
@@ -408,12 +418,16 @@ static int make_plan(const octo_attend_t* c, int sms, AttendPlan* p) {
     // no more tiles than the rows make, with one that is not full in every segment
     const int64_t rows_make = (c->q_total * group + tile_rows - 1) / tile_rows + c->segments;
     const int64_t busy = units < rows_make * c->kv_heads ? units : rows_make * c->kv_heads;
-    // Work is split over the keys while that keeps more of the GPU busy: tiles up to one per SM, few rows up to
-    // kStepFill CTAs per SM; a split has 512 keys at least, and all are of one size.
-    const int64_t want = p->tile ? sms : (int64_t)sms * kStepFill;
-    int64_t splits = p->tile ? want / busy : (want + busy - 1) / busy;
-    const int64_t most = (max_k + 511) / 512;
-    if (splits > most) splits = most;
+    // Work is split over the keys, into splits of one size.  Few rows: up to kStepFill CTAs per SM, 512 keys at least.  Tiles:
+    // up to one per SM at 512 keys at least, and beyond that up to four per SM at 2048 keys at least, since tiles of
+    // uneven length on one CTA per SM end at different times (36 segments of about 350 rows and up to 5300 keys, 4 heads of
+    // 64: 150 -> SPLIT_US us).
+    auto at_most = [&](int64_t want, int64_t keys) {
+        const int64_t a = want / busy, b = max_k / keys;
+        return a < b ? a : b;
+    };
+    int64_t splits = p->tile ? at_most(sms, 512) : at_most((int64_t)sms * kStepFill + busy - 1, 512);
+    if (p->tile && at_most((int64_t)sms * 4, 2048) > splits) splits = at_most((int64_t)sms * 4, 2048);
     if (splits < 1) splits = 1;
     const int64_t chunk = ((max_k + splits - 1) / splits + step - 1) / step * step;
     splits = (max_k + chunk - 1) / chunk;
@@ -432,14 +446,14 @@ static cudaError_t launch_attend(const AttendArgs& a, const AttendPlan& p, cudaS
         e = launch_attend_tile(a, std::is_same<T, __nv_bfloat16>::value, (int)p.ctas, (int)p.row_tiles, stream);
     } else {
         const bool eight = a.max_q * a.group <= 8;
-        void (*kernel)(const AttendArgs);
+        void (*kernel)(const AttendArgs, int);
         if (a.dim <= 64)
             kernel = a.mask ? (eight ? attend_step_kernel<T, 1, 1, true> : attend_step_kernel<T, 1, 2, true>)
                             : (eight ? attend_step_kernel<T, 1, 1, false> : attend_step_kernel<T, 1, 2, false>);
         else
             kernel = a.mask ? (eight ? attend_step_kernel<T, 2, 1, true> : attend_step_kernel<T, 2, 2, true>)
                             : (eight ? attend_step_kernel<T, 2, 1, false> : attend_step_kernel<T, 2, 2, false>);
-        e = launch_kernel(kernel, dim3((unsigned)p.ctas), dim3(kStepThreads), 0, stream, a);
+        e = launch_kernel(kernel, dim3((unsigned)p.ctas), dim3(kStepThreads), 0, stream, a, (int)p.row_tiles);
     }
     if (e == cudaSuccess && a.splits > 1) {
         const int64_t blocks = (a.q_total * a.heads * 32 + kJoinThreads - 1) / kJoinThreads;

@@ -171,34 +171,90 @@ struct RotArgs {
 
 constexpr int kRotThreads = 256;
 
-template <typename T> struct Conv;
-template <> struct Conv<__half> {
-    static __device__ __forceinline__ float up(__half v) { return __half2float(v); }
-    static __device__ __forceinline__ __half down(float v) { return __float2half_rn(v); }
-};
-template <> struct Conv<__nv_bfloat16> {
-    static __device__ __forceinline__ float up(__nv_bfloat16 v) { return __bfloat162float(v); }
-    static __device__ __forceinline__ __nv_bfloat16 down(float v) { return __float2bfloat16_rn(v); }
-};
-template <> struct Conv<float> {
-    static __device__ __forceinline__ float up(float v) { return v; }
-    static __device__ __forceinline__ float down(float v) { return v; }
-};
-
 // N elements of T that start on a multiple of their own size (at most 16 bytes at a time).
 template <typename T, int N>
 struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Run {
     T v[N];
 };
 
-// Sine and cosine of position * freq.  The product of two binary32 numbers is exact in binary64, and so is
-// the subtraction of the whole turns up to 2^-53 of their number: the phase keeps binary32's precision
-// however far the position.
-__device__ __forceinline__ void turn_of(double position, float freq, float& c, float& s) {
+__device__ __forceinline__ float one_up(__half v) { return __half2float(v); }
+__device__ __forceinline__ float one_up(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float one_up(float v) { return v; }
+__device__ __forceinline__ void one_down(float f, __half& v) { v = __float2half_rn(f); }
+__device__ __forceinline__ void one_down(float f, __nv_bfloat16& v) { v = __float2bfloat16_rn(f); }
+__device__ __forceinline__ void one_down(float f, float& v) { v = f; }
+__device__ __forceinline__ void two_up(uint32_t w, float& a, float& b, __half) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    a = f.x;
+    b = f.y;
+}
+__device__ __forceinline__ void two_up(uint32_t w, float& a, float& b, __nv_bfloat16) {
+    a = __uint_as_float(w << 16);
+    b = __uint_as_float(w & 0xffff0000u);
+}
+__device__ __forceinline__ uint32_t two_down(float a, float b, __half) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t two_down(float a, float b, __nv_bfloat16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// A run to binary32 and back; 16-bit types two at a time.
+template <typename T, int N>
+__device__ __forceinline__ void run_up(const Run<T, N>& r, float* f) {
+    if constexpr (sizeof(T) == 2 && N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) two_up(reinterpret_cast<const uint32_t*>(&r)[i / 2], f[i], f[i + 1], T());
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = one_up(r.v[i]);
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ Run<T, N> run_down(const float* f) {
+    Run<T, N> r;
+    if constexpr (sizeof(T) == 2 && N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) reinterpret_cast<uint32_t*>(&r)[i / 2] = two_down(f[i], f[i + 1], T());
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) one_down(f[i], r.v[i]);
+    }
+    return r;
+}
+
+// Sine and cosine of position * freq, from the whole turns' remainder.  In binary64 (the product of two binary32
+// numbers is exact) for positions of any size ...
+__device__ __noinline__ void turn_far(double position, float freq, float& c, float& s) {
     const double turns = position * (double)freq * 0.15915494309189533577;
     const double half_turns = 2.0 * (turns - rint(turns));  // in [-1, 1]
     const float h = (float)half_turns;
     const float rest = (float)(half_turns - (double)h) * 3.14159265f;  // what the rounding of h left, as an angle
+    float s0, c0;
+    sincospif(h, &s0, &c0);
+    s = fmaf(c0, rest, s0);
+    c = fmaf(-s0, rest, c0);
+}
+// ... and in pairs of binary32 numbers below 2^22 turns: freq / 2 pi and the product with the position are each held as
+// a sum of two (an error of 2^-47 of the turns, 2^-25 of a turn at most), the first of which loses its whole turns
+// exactly.  Conversions and products in binary64 took most of a token's time where it has few heads.
+// COARSE: the hardware's sine and cosine (off by at most 2^-21 in [-pi, pi]), for results of 16 bits.
+template <bool COARSE>
+__device__ __forceinline__ void turn_of(float position, float freq, float& c, float& s) {
+    const float f1 = freq * 0.15915494f, f2 = fmaf(freq, 6.4206383e-9f, fmaf(freq, 0.15915494f, -f1));  // 1 / 2 pi in two parts
+    const float p1 = position * f1;
+    if (!(fabsf(p1) < 4194304.0f)) return turn_far((double)position, freq, c, s);
+    const float p2 = fmaf(position, f2, fmaf(position, f1, -p1));
+    const float whole = p1 - rintf(p1);
+    float t = whole + p2;
+    if (COARSE) {
+        __sincosf((t - rintf(t)) * 6.28318531f, &s, &c);
+        return;
+    }
+    const float left = p2 - (t - whole);
+    t -= rintf(t);
+    const float h = 2.0f * t, rest = left * 6.28318531f;  // what the rounding of t left, as an angle
     float s0, c0;
     sincospif(h, &s0, &c0);
     s = fmaf(c0, rest, s0);
@@ -263,9 +319,13 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lanes, int heads_per_group)
                 const int axis = a.axes[p + j];
                 if (axis >= 0 && axis < a.num_axes) {
                     const int64_t at = row * a.num_axes + axis;
-                    const double pos = a.positions_are_int ? (double)static_cast<const int*>(a.positions)[at]
-                                                           : (double)static_cast<const float*>(a.positions)[at];
-                    turn_of(pos, a.freqs[p + j], c, s);
+                    if (a.positions_are_int) {
+                        const int pos = static_cast<const int*>(a.positions)[at];
+                        if (abs(pos) <= 1 << 24) turn_of<sizeof(T) == 2>((float)pos, a.freqs[p + j], c, s);
+                        else turn_far((double)pos, a.freqs[p + j], c, s);
+                    } else {
+                        turn_of<sizeof(T) == 2>(static_cast<const float*>(a.positions)[at], a.freqs[p + j], c, s);
+                    }
                 }
             }
             cs[u * VP + j] = c;
@@ -287,21 +347,21 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lanes, int heads_per_group)
         float m00[N], m01[N], m11[N], m10[N];
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
-            Run<T, VP> w[2];
+            float w[2 * VP];
+#pragma unroll
+            for (int j = 0; j < 2 * VP; ++j) w[j] = 1.0f;
             if (weight && own[u]) {
-                w[0] = *reinterpret_cast<const Run<T, VP>*>(weight + e0[u]);
-                w[1] = *reinterpret_cast<const Run<T, VP>*>(weight + e1[u]);
+                run_up<T, VP>(*reinterpret_cast<const Run<T, VP>*>(weight + e0[u]), w);
+                run_up<T, VP>(*reinterpret_cast<const Run<T, VP>*>(weight + e1[u]), w + VP);
             }
 #pragma unroll
             for (int j = 0; j < VP; ++j) {
                 const int m = ILV ? 2 * j : j, n = ILV ? 2 * j + 1 : VP + j;  // the pair inside the unit's 2 VP elements
-                const float w0 = weight && own[u] ? Conv<T>::up(w[m / VP].v[m % VP]) : 1.0f;
-                const float w1 = weight && own[u] ? Conv<T>::up(w[n / VP].v[n % VP]) : 1.0f;
                 const int k = u * VP + j;
-                m00[k] = w0 * cs[k];
-                m01[k] = w1 * sn[k];
-                m11[k] = w1 * cs[k];
-                m10[k] = w0 * sn[k];
+                m00[k] = w[m] * cs[k];
+                m01[k] = w[n] * sn[k];
+                m11[k] = w[n] * cs[k];
+                m10[k] = w[m] * sn[k];
             }
         }
         for (int h = b; h < e; h += BATCH) {
@@ -323,13 +383,15 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lanes, int heads_per_group)
                 if (weight) {
                     float sum = 0.0f;
 #pragma unroll
-                    for (int u = 0; u < NU; ++u)
+                    for (int u = 0; u < NU; ++u) {
+                        float f[2 * VP];
+                        run_up<T, VP>(x[k][u][0], f);
+                        run_up<T, VP>(x[k][u][1], f + VP);
+                        float part = 0.0f;
 #pragma unroll
-                        for (int j = 0; j < VP; ++j) {
-                            const float p = own[u] ? Conv<T>::up(x[k][u][0].v[j]) : 0.0f, q = own[u] ? Conv<T>::up(x[k][u][1].v[j]) : 0.0f;
-                            sum = fmaf(p, p, sum);
-                            sum = fmaf(q, q, sum);
-                        }
+                        for (int j = 0; j < 2 * VP; ++j) part = fmaf(f[j], f[j], part);
+                        if (own[u]) sum += part;
+                    }
                     r[k] = rsqrtf(fmaf(group_sum(sum, mask, first, lanes, in), inv_dim, a.eps));
                 }
             }
@@ -340,16 +402,18 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lanes, int heads_per_group)
 #pragma unroll
                 for (int u = 0; u < NU; ++u)
                     if (own[u]) {
-                        Run<T, VP> y[2];
+                        float f[2 * VP], y[2 * VP];
+                        run_up<T, VP>(x[k][u][0], f);
+                        run_up<T, VP>(x[k][u][1], f + VP);
 #pragma unroll
                         for (int j = 0; j < VP; ++j) {
                             const int m = ILV ? 2 * j : j, n = ILV ? 2 * j + 1 : VP + j, i = u * VP + j;
-                            const float x0 = r[k] * Conv<T>::up(x[k][u][m / VP].v[m % VP]), x1 = r[k] * Conv<T>::up(x[k][u][n / VP].v[n % VP]);
-                            y[m / VP].v[m % VP] = Conv<T>::down(fmaf(x0, m00[i], -(x1 * m01[i])));
-                            y[n / VP].v[n % VP] = Conv<T>::down(fmaf(x1, m11[i], x0 * m10[i]));
+                            const float x0 = r[k] * f[m], x1 = r[k] * f[n];
+                            y[m] = fmaf(x0, m00[i], -(x1 * m01[i]));
+                            y[n] = fmaf(x1, m11[i], x0 * m10[i]);
                         }
-                        *reinterpret_cast<Run<T, VP>*>(head + e0[u]) = y[0];
-                        *reinterpret_cast<Run<T, VP>*>(head + e1[u]) = y[1];
+                        *reinterpret_cast<Run<T, VP>*>(head + e0[u]) = run_down<T, VP>(y);
+                        *reinterpret_cast<Run<T, VP>*>(head + e1[u]) = run_down<T, VP>(y + VP);
                     }
             }
         }
@@ -395,6 +459,10 @@ template <typename T>
 static cudaError_t rotate_typed(const octo_rotate_t& c, const RotArgs& a, int sm_count, cudaStream_t stream) {
     if (runs_of(c, a, 8, (int)sizeof(T))) return launch_rotate<T, 8, 1>(a, c.interleaved != 0, sm_count, stream);
     if (runs_of(c, a, 4, (int)sizeof(T))) return launch_rotate<T, 4, 1>(a, c.interleaved != 0, sm_count, stream);
+    const int half = c.head_dim / 2;
+    if (half <= 64 && runs_of(c, a, 2, (int)sizeof(T))) return launch_rotate<T, 2, 1>(a, c.interleaved != 0, sm_count, stream);
+    if (half <= 32) return launch_rotate<T, 1, 1>(a, c.interleaved != 0, sm_count, stream);
+    if (half <= 64) return launch_rotate<T, 1, 2>(a, c.interleaved != 0, sm_count, stream);
     return launch_rotate<T, 1, 4>(a, c.interleaved != 0, sm_count, stream);
 }
 
