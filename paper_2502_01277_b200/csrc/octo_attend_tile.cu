@@ -774,22 +774,52 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                 };
                 if (mask) look_ahead();
                 for (bool last = false; !last && !ld.dead; ++tile) {
-                    // the next 128 visible keys
-                    int take, from = cursor;
+                    // The next 128 visible keys: those that are listed, and then the keys that follow without a gap where there
+                    // are enough of them (the states of a frame between its canvas bands); else the list is filled up.
+                    int take, from = cursor, kept = 0;  // rows below `kept` from the list, the others from `from` on
                     if (mask) {
-                        while (listed <= kHalf && cursor < it.ke) {  // (at most 128 are listed here, and 128 more fit)
+                        bool gapless = false;
+                        while (listed <= kHalf) {
+                            unsigned ballot[4];
+                            bool all = true;
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                const unsigned ballot = __ballot_sync(0xffffffffu, seen[j]);
-                                if (seen[j]) list[listed + __popc(ballot & ((1u << lane) - 1u))] = cursor + 32 * j + lane;
-                                listed += __popc(ballot);
+                                ballot[j] = __ballot_sync(0xffffffffu, seen[j]);
+                                const int wanted = min(max(kHalf - listed - 32 * j, 0), 32);  // of these 32
+                                const unsigned those = wanted == 32 ? 0xffffffffu : (1u << wanted) - 1u;
+                                all = all && (ballot[j] & those) == those;
                             }
-                            cursor += 128;
+                            gapless = all && listed < kHalf;
+                            if (gapless || cursor >= it.ke) break;
+                            const int hidden = ballot[0] ? __ffs(ballot[0]) - 1 : 32;
+                            if (listed == 0 && hidden > 0) {  // begin at a visible key
+                                cursor += ballot[0] | ballot[1] | ballot[2] | ballot[3] ? hidden : 128;
+                            } else {  // (at most 128 are listed here, and 128 more fit)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    if (seen[j]) list[listed + __popc(ballot[j] & ((1u << lane) - 1u))] = cursor + 32 * j + lane;
+                                    listed += __popc(ballot[j]);
+                                }
+                                cursor += 128;
+                            }
                             look_ahead();
                         }
                         __syncwarp();
-                        take = min(listed, kHalf);
-                        last = listed <= kHalf;
+                        kept = gapless ? listed : kHalf;
+                        take = gapless ? kHalf : min(listed, kHalf);
+                        from = cursor;
+                        if (gapless) {  // is there any key left?
+                            cursor += kHalf - listed;
+                            look_ahead();
+                            while (!__any_sync(0xffffffffu, seen[0] || seen[1] || seen[2] || seen[3]) && cursor < it.ke) {
+                                cursor += 128;
+                                look_ahead();
+                            }
+                            last = cursor >= it.ke;
+                            listed = take;  // (none is left over)
+                        } else {
+                            last = listed <= kHalf;
+                        }
                     } else {
                         take = min(it.ke - cursor, kHalf);
                         cursor += take;
@@ -804,7 +834,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                         const char* const src = which ? v : k;
                         const int stride = (int)(2 * (which ? a.v_row : a.k_row));
                         const uint32_t dst = ring + (n % Shape::kStages) * Shape::kStageBytes;
-                        if (mask) ld.tile(dst, take, src, stride, [&](int r) { return list[r]; });
+                        if (mask && kept > 0) ld.tile(dst, take, src, stride, [&](int r) { return r < kept ? list[r] : from + r - kept; });
                         else if (take == kHalf && OCTO_TOKEN_IN_RANGE(from >= 0 && from + kHalf <= it.ke, a.status)) ld.full_tile(dst, src + (int64_t)from * stride, stride);
                         else ld.tile(dst, take, src, stride, [&](int r) { return from + r; });
                         ld.issued(&sh->full[n % Shape::kStages]);

@@ -575,3 +575,15 @@ def test_attention_one_wide_head_for_many_queries():
     k = base[:, :1]
     _attend_check(q, k, k, 2, q_rows=3, k_rows=250)
     _attend_check(q.transpose(0, 1).contiguous().transpose(0, 1), base[:, 1:2], base[:, 2:], 6, q_rows=1, k_rows=83)
+
+
+@pytest.mark.parametrize("q_rows,dim", [(3, 64), (140, 64), (60, 128), (300, 128)])
+@pytest.mark.parametrize("period,edge", [(1600, 350), (100, 3), (129, 1), (128, 0), (64, 31), (257, 128), (1000, 499)])
+def test_attention_banded_masks(q_rows, dim, period, edge):
+    """Visible keys in runs (frames between their canvas bands): runs longer and shorter than a tile, single keys between."""
+    q, k, v = _qkv(period, 2 * q_rows, 2 * 3333, 2, 1, dim, BF16)
+    place = torch.arange(k.shape[0], device="cuda") % period
+    mask = ((place >= edge) & (place < period - edge)).to(torch.uint8)
+    k[mask == 0], v[mask == 0] = math.nan, math.nan
+    _attend_check(q, k, v, 2, q_rows=q_rows, k_rows=3333, key_mask=mask)
+    _attend_check(q, k, v, 3, q_rows=q_rows, k_offsets=_ints([5, 6, 3000, 6666]), key_mask=mask)
