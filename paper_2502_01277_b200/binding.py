@@ -377,6 +377,17 @@ def _stream_getter(torch, device):
     return lambda: raw(index)
 
 
+def _empty(torch, shape, dtype, device, stream):
+    """An uninitialised tensor that a call on `stream` (None: the current one) fills.  It is made on that stream, since
+    memory that the current stream has let go of may still be in use there, and marked as read on the current one."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        made = torch.empty(shape, dtype=dtype, device=device)
+    made.record_stream(torch.cuda.current_stream(device))
+    return made
+
+
 class Stage:
     """Owns one octo_stage_t and the torch tensors a caller usually wants around it."""
 
@@ -530,9 +541,9 @@ class Stage:
                                   or times.device != self.device):
             raise OctoError(OCTO_E_INVALID_ARG, "octo_stage_patch_positions (times is not a float32 vector, one per frame)")
         if positions is None:
-            positions = t.empty((max_items, patches, 3), dtype=t.float32, device=self.device)
+            positions = _empty(t, (max_items, patches, 3), t.float32, self.device, stream)
         if visible is None:
-            visible = t.empty((max_items, patches), dtype=t.uint8, device=self.device)
+            visible = _empty(t, (max_items, patches), t.uint8, self.device, stream)
         for b, dtype, count in ((positions, t.float32, 3 * max_items * patches), (visible, t.uint8, max_items * patches)):
             if b.dtype != dtype or b.numel() < count or not b.is_contiguous() or b.device != self.device:
                 raise OctoError(OCTO_E_INVALID_ARG, "octo_stage_patch_positions (an output has another shape)")

@@ -3,7 +3,9 @@ packed crops, norm and rotation of query and key heads, attention to another set
 
 Argument checks and marshalling only; the work is done by octo_patch_positions, octo_norm_rotate and
 octo_cross_attention of the C ABI (include/octo.h has the rules).  Calls enqueue on the current stream of the
-tensors' device, or on `stream`; nothing synchronises, and a call may be captured into a CUDA graph."""
+tensors' device, or on `stream`; nothing synchronises, and a call may be captured into a CUDA graph.  What a call
+allocates belongs to the stream it runs on; inputs have to be ready there.  There is no backward pass: results
+carry no gradient history."""
 from __future__ import annotations
 
 import ctypes
@@ -76,9 +78,9 @@ def patch_positions(items, slot: Tuple[int, int], patch: int, *, keep_aspect: bo
         _refuse(where, "the patch does not divide the slot")
     dev, patches = items.device, (w // patch) * (h // patch)
     if positions is None:
-        positions = t.empty((n, patches, 3), dtype=t.float32, device=dev)
+        positions = B._empty(t, (n, patches, 3), t.float32, dev, stream)
     if visible is None:
-        visible = t.empty((n, patches), dtype=t.uint8, device=dev)
+        visible = B._empty(t, (n, patches), t.uint8, dev, stream)
     if positions.dtype is not t.float32 or not positions.is_contiguous() or positions.numel() != n * patches * 3:
         _refuse(where, "positions has another shape")
     if visible.dtype is not t.uint8 or not visible.is_contiguous() or visible.numel() != n * patches:
@@ -119,8 +121,8 @@ def norm_rotate(q, k, positions, freqs, axes, *, q_weight=None, k_weight=None, e
             _refuse(where, "k does not fit q")
         kv = k.shape[1]
     if out is None:
-        out = (t.empty((rows, heads, dim), dtype=dtype, device=dev),
-               None if k is None else t.empty((rows, kv, dim), dtype=dtype, device=dev))
+        out = (B._empty(t, (rows, heads, dim), dtype, dev, stream),
+               None if k is None else B._empty(t, (rows, kv, dim), dtype, dev, stream))
     q_out, k_out = out
     views = []
     for x, y in ((q, q_out), (k, k_out)):
@@ -182,7 +184,7 @@ def cross_attention(q, k, v, segments: int, *, q_offsets=None, k_offsets=None, q
     if kv == 0 or heads % kv:
         _refuse(where, "kv_heads does not divide heads")
     if out is None:
-        out = t.empty((q_total, heads, dim), dtype=dtype, device=dev)
+        out = B._empty(t, (q_total, heads, dim), dtype, dev, stream)
     elif out.shape != q.shape or out.dtype is not dtype:
         _refuse(where, "out has another shape")
     views = []
@@ -213,11 +215,7 @@ def cross_attention(q, k, v, segments: int, *, q_offsets=None, k_offsets=None, q
     rc = lib.octo_attend_workspace(args, ctypes.byref(need))
     if rc != B.OCTO_OK:
         raise B.OctoError(rc, "octo_attend_workspace")
-    workspace = None
-    if need.value:
-        workspace = t.empty((need.value,), dtype=t.uint8, device=dev)
-        if stream is not None:
-            workspace.record_stream(stream)
+    workspace = B._empty(t, (need.value,), t.uint8, dev, stream) if need.value else None
     rc = lib.octo_cross_attention(args, None if workspace is None else workspace.data_ptr(), need.value, _stream_of(dev, stream))
     if rc != B.OCTO_OK:
         raise B.OctoError(rc, "octo_cross_attention")

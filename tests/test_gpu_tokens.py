@@ -587,3 +587,30 @@ def test_attention_banded_masks(q_rows, dim, period, edge):
     k[mask == 0], v[mask == 0] = math.nan, math.nan
     _attend_check(q, k, v, 2, q_rows=q_rows, k_rows=3333, key_mask=mask)
     _attend_check(q, k, v, 3, q_rows=q_rows, k_offsets=_ints([5, 6, 3000, 6666]), key_mask=mask)
+
+
+def test_results_on_another_stream_are_not_taken_from_memory_in_use():
+    """What a call on a given stream allocates is that stream's: memory that the current stream has let go of may still
+    be written by work under way there."""
+    g = _gen(11)
+    q, k, v = _qkv(11, 1, 20000, 8, 1, 64, BF16)
+    items = torch.zeros((64, 8), dtype=torch.int32, device="cuda")
+    items[:, 4:6] = 100
+    pos = torch.rand((64, 1), generator=g, device="cuda") * 100
+    freqs, axes = torch.rand(32, generator=g, device="cuda"), torch.zeros(32, dtype=torch.int32, device="cuda")
+    x = torch.randn((64, 4, 64), generator=g, device="cuda").to(BF16)
+    calls = [lambda st: (octo.cross_attention(q, k, v, 1, k_rows=20000, stream=st),),
+             lambda st: octo.norm_rotate(x, x[:, :2], pos, freqs, axes, stream=st),
+             lambda st: octo.patch_positions(items, (224, 224), 16, stream=st)]
+    side = torch.cuda.Stream()
+    for call in calls:
+        want = call(None)
+        torch.cuda.synchronize()
+        in_use = [torch.empty_like(w) for w in want for _ in range(3)]
+        torch.cuda._sleep(100_000_000)
+        for b in in_use:
+            b.fill_(77)
+        del in_use, b
+        got = call(side)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
