@@ -295,7 +295,7 @@ struct Loader {
     // 128 rows that lie side by side from `src` on.
     __device__ __forceinline__ void full_tile(uint32_t dst, const char* src, int stride) {
         const char* p = wide ? src + (int64_t)(8 * warp + own()) * stride + column() * 16 : zero_row;
-        const int64_t turn = wide ? kRowsAtOnce * stride : 0, group = wide ? (int64_t)(8 * kLoadWarps) * stride : 0;
+        const int64_t turn = wide ? (int64_t)kRowsAtOnce * stride : 0, group = wide ? (int64_t)(8 * kLoadWarps) * stride : 0;
         uint32_t at = dst + (uint32_t)warp * 1024u;
 #pragma unroll 4
         for (int g = 0; g < kGroups; ++g) {

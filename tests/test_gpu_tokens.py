@@ -614,3 +614,23 @@ def test_results_on_another_stream_are_not_taken_from_memory_in_use():
         got = call(side)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_attention_rows_half_a_gigabyte_apart():
+    """Four rows of such a tensor are 2^31 bytes."""
+    apart, k_total, q_rows, dim = (1 << 28) + 8, 128, 34000, 64
+    if torch.cuda.mem_get_info()[0] < 2 * apart * k_total + (4 << 30):
+        pytest.skip("needs 73 GB of device memory")
+    store = torch.empty(apart * k_total, dtype=BF16, device="cuda")
+    k = torch.as_strided(store, (k_total, 1, dim), (apart, dim, 1), 0)
+    v = torch.as_strided(store, (k_total, 1, dim), (apart, dim, 1), 1024)
+    g = _gen(12)
+    k.copy_(torch.randn((k_total, 1, dim), generator=g, device="cuda"))
+    v.copy_(torch.randn((k_total, 1, dim), generator=g, device="cuda"))
+    q = torch.randn((q_rows, 1, dim), generator=g, device="cuda").to(BF16)
+    _attend_check(q, k, v, 1, q_rows=q_rows, k_rows=k_total)
+    mask = torch.ones(k_total, dtype=torch.uint8, device="cuda")
+    mask[7] = 0
+    _attend_check(q, k, v, 1, q_rows=q_rows, k_rows=k_total, key_mask=mask)
+    del store, k, v
+    torch.cuda.empty_cache()
