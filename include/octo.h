@@ -508,8 +508,9 @@ typedef struct {
  * For a head x of head_dim elements: y = x * rsqrt(mean(x^2) + eps) * weight (no weight: y = x); then pair i
  * of the first 2 * pairs elements, (i, i + pairs) or with `interleaved` (2 i, 2 i + 1), is turned by the angle
  * position[axis[i]] * freq[i]: (y0 cos - y1 sin, y1 cos + y0 sin); elements from 2 * pairs on stay y.
- * The angle is reduced in 64 bits (a position of 2^24 and a frequency of 1 still have a phase that is good to
- * binary32); everything else is binary32, rounded once to the type of the tensors.
+ * The angle is reduced in 46 bits or more (a position of 2^24 and a frequency of 1 still have a phase that is good
+ * to binary32); everything else is binary32, rounded once to the type of the tensors.  For the 16-bit types sine
+ * and cosine are off by up to 2^-21.
  */
 typedef struct {
     int32_t device, dtype;            /* OCTO_F16, OCTO_BF16 or OCTO_F32                                   */
@@ -554,7 +555,7 @@ typedef struct {
     int32_t heads, kv_heads;          /* kv_heads divides heads                                            */
     int32_t head_dim;                 /* a multiple of 8, 8 .. 128                                         */
     int64_t q_total, k_total;         /* rows of q and out; rows of k, v and the mask: at most 2^30, and   */
-                                      /* q_total * heads < 2^31                                            */
+                                      /* q_total * heads at most 2^31 - 512                                */
     octo_heads_t q, k, v, out;        /* 16-byte aligned; strides multiples of 8 elements, 0 .. 2^30 - 8    */
     const int32_t* d_q_offsets;       /* [segments + 1] non-decreasing, or NULL                            */
     const int32_t* d_k_offsets;       /* [segments + 1] non-decreasing, or NULL                            */
@@ -571,8 +572,8 @@ typedef struct {
 
 #define OCTO_MAX_SEGMENTS 2048
 
-/* Bytes of workspace that octo_cross_attention needs for these arguments (pointers are not looked at); 0 where
- * no work is split over the keys. */
+/* Bytes of workspace that octo_cross_attention needs for these arguments (of the pointers it only matters which
+ * offsets are NULL); 0 where no work is split over the keys. */
 OCTO_API int octo_attend_workspace(const octo_attend_t* args, int64_t* bytes);
 
 /* d_workspace: device, at least that many bytes, 16-byte aligned; its contents mean nothing between calls.

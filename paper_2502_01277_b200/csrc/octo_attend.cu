@@ -383,7 +383,7 @@ static int validate(const octo_attend_t* c) {
     if (c->head_dim < 8 || c->head_dim > 128 || c->head_dim % 8) return OCTO_E_INVALID_ARG;
     const int64_t most = 1 << 30;
     if (c->q_total < 0 || c->k_total < 0 || c->q_total > most || c->k_total > most) return OCTO_E_INVALID_ARG;
-    if (c->q_total * c->heads > INT32_MAX) return OCTO_E_CAPACITY;
+    if (c->q_total * c->heads > INT32_MAX - 511) return OCTO_E_CAPACITY;  // rows of the last tile are numbered in 32 bits too
     if (c->q_rows < 1 || c->k_rows < 1 || c->q_rows > most || c->k_rows > most) return OCTO_E_INVALID_ARG;
     if (c->q_first < -most || c->q_first > most || c->k_first < -most || c->k_first > most) return OCTO_E_INVALID_ARG;
     if (c->max_q < 0 || c->max_k < 0) return OCTO_E_INVALID_ARG;

@@ -143,3 +143,13 @@ def test_host_tensors_are_refused(call):
     with pytest.raises(octo.OctoError) as e:
         call()
     assert e.value.code == B.OCTO_E_INVALID_ARG
+
+
+@pytest.mark.parametrize("heads,kv_heads,q_total", [(256, 1, (1 << 23) - 1), (256, 256, (1 << 23) - 1), (1, 1, 1 << 30),
+                                                    (2, 1, (1 << 30) - 1)])
+def test_attention_refuses_rows_that_32_bits_cannot_number(lib, heads, kv_heads, q_total):
+    """Rows of a tile are numbered up to 255 beyond the last."""
+    fits = q_total * heads <= (1 << 31) - 512
+    need = ctypes.c_int64(7)
+    rc = lib.octo_attend_workspace(ctypes.byref(_attend(heads=heads, kv_heads=kv_heads, q_total=q_total)), ctypes.byref(need))
+    assert (rc != B.OCTO_E_CAPACITY) == fits and need.value == 0
