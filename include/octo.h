@@ -491,8 +491,9 @@ OCTO_API int octo_patch_positions(int32_t device, const octo_item_t* d_items, in
                                   void* cuda_stream);
 
 /* The same for the crops that the last octo_crop_batch of `branch` packed: its item table, its packed count,
- * its slot size and fit.  max_items as in that call (or fewer).  d_times: one time per frame of the batch, or
- * NULL.  Errors: as above, plus OCTO_E_NO_POSTPROCESS (the branch has not been cropped yet). */
+ * its slot size and fit.  max_items as in that call (or fewer).  The d_n_items of that call is read again, on the
+ * device: it stays valid and unchanged until this has run.  d_times: one time per frame of the batch, or NULL.
+ * Errors: as above, plus OCTO_E_NO_POSTPROCESS (the branch has not been cropped yet). */
 OCTO_API int octo_stage_patch_positions(octo_stage_t* st, int32_t branch, int32_t max_items, int32_t patch,
                                         const float* d_times, float* d_positions, uint8_t* d_visible,
                                         void* cuda_stream);

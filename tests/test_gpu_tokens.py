@@ -634,3 +634,45 @@ def test_attention_rows_half_a_gigabyte_apart():
     _attend_check(q, k, v, 1, q_rows=q_rows, k_rows=k_total, key_mask=mask)
     del store, k, v
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("first_item,cap", [(0, 5), (5, 7), (3, 1000), (100000, 8)])
+def test_windows_of_a_branch(first_item, cap):
+    """Positions of a window of a branch's items, and attention of its tokens (the offsets count all items)."""
+    import workloads
+    from gpu_harness import make_stage, upload_frames
+    b = workloads.make_batch("two_branch", batch=3)
+    wl = b.workload
+    st = make_stage(wl, b.n, branches=((224, 224), (64, 32)))
+    frames, head = upload_frames(b.frames), torch.from_numpy(b.head).cuda()
+    st.preprocess(frames, b.sizes)
+    st.postprocess(head)
+    _, offsets, n_items = st.crop(0, cap, first_item=first_item)
+    pos = torch.full((cap, 196, 3), -5.0, device="cuda")
+    vis = torch.full((cap, 196), 9, dtype=torch.uint8, device="cuda")
+    st.patch_positions(0, cap, 16, positions=pos, visible=vis)
+    packed, total = n_items.tolist()
+    assert packed == max(0, min(cap, total - first_item)) and total > 12
+    table = st.item_table(0, packed) if packed else None
+    if packed:
+        rec = np.stack([table[f] for f in ("frame", "det", "rx0", "ry0", "rx1", "ry1")], 1)
+        want, wvis = _positions_ref(rec, (224, 224), 16, 0, None)
+        got = pos[:packed].cpu().numpy().astype(np.float64)
+        assert (np.abs(got - want) <= 2.0**-24 * np.abs(want) * (1 + 1e-6) + 1e-9).all()
+        assert np.array_equal(vis[:packed].cpu().numpy(), wvis)
+    assert (pos[packed:] == -5).all() and (vis[packed:] == 9).all()
+    tokens, states = 3, 70
+    g = _gen(first_item)
+    q = torch.randn((cap * tokens, 4, 64), generator=g, device="cuda").to(BF16)
+    k, v = (torch.randn((b.n * states, 2, 64), generator=g, device="cuda").to(BF16) for _ in range(2))
+    out = torch.full_like(q, 7.0)
+    octo.cross_attention(q, k, v, b.n, q_offsets=offsets, q_rows=tokens, k_rows=states, q_first=first_item, out=out)
+    assert (out[packed * tokens:] == 7).all()
+    for i in range(packed):  # every item to the states of its own frame
+        f = int(table["frame"][i])
+        one = slice(i * tokens, (i + 1) * tokens)
+        ref, size, plain, _ = _attend_ref(q[one], k[f * states:(f + 1) * states], v[f * states:(f + 1) * states], 1,
+                                          q_rows=tokens, k_rows=states)
+        tol = (2 * _u(BF16) + 2.0**-15) * size + 2.0**-25 * (plain + 1)
+        assert ((out[one].double() - ref).abs() <= tol).all()
+    st.close()
