@@ -3,7 +3,9 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "octo_tokens.h"
 
@@ -275,11 +277,17 @@ __device__ __forceinline__ float group_sum(float v, unsigned mask, int first, in
     return __shfl_sync(mask, v, first);
 }
 
-// ILV: pairs are neighbours.  `lanes` lanes per token, NU units of VP pairs per lane.
-template <typename T, int VP, int NU, bool ILV>
-__global__ void __launch_bounds__(kRotThreads, 2)
+// CTAs an SM should hold: many where few heads are in flight, since the wait for a token's angles and heads is then
+// covered by other tokens.
+template <typename T, int VP, int NU, int BATCH>
+constexpr int rotate_ctas() {
+    return BATCH * VP >= 4 * 8 || sizeof(T) * VP * NU * BATCH >= 64 ? 2 : (sizeof(T) * VP * NU > 16 ? 3 : 4);
+}
+
+// ILV: pairs are neighbours.  `lanes` lanes per token, NU units of VP pairs per lane, BATCH heads of a group in flight together.
+template <typename T, int VP, int NU, bool ILV, int BATCH>
+__global__ void __launch_bounds__(kRotThreads, rotate_ctas<T, VP, NU, BATCH>())
 rotate_kernel(const __grid_constant__ RotArgs a, int lanes, int heads_per_group) {
-    constexpr int BATCH = sizeof(T) * VP * NU <= 16 ? 4 : 2;  // heads of a group that are in flight together
     constexpr int N = VP * NU;
     pdl_wait();
     const int lane = threadIdx.x & 31, tokens = 32 / lanes, mine = lane / lanes, in = lane - mine * lanes;
@@ -437,8 +445,20 @@ static cudaError_t launch_rotate(const RotArgs& a, bool interleaved, int sm_coun
     }
     const int64_t blocks = (warps + kRotThreads / 32 - 1) / (kRotThreads / 32);
     const dim3 grid((unsigned)blocks, (unsigned)ceil_div(total, per));
-    auto kernel = interleaved ? rotate_kernel<T, VP, NU, true> : rotate_kernel<T, VP, NU, false>;
-    return launch_kernel(kernel, grid, dim3(kRotThreads), 0, stream, a, lanes, per);
+    // Heads in flight.  One head: one.  Runs of less than eight elements, or few heads: two, and more CTAs (us two / four:
+    // 137 000 tokens, 16 + 16 heads of 72 314 / 363; 196 000 tokens, 5 + 5 heads of 64 124 / 138).  Else what 16 registers of
+    // a lane hold (four of 16 bits, two of binary32; 274 000 tokens, 16 + 16 heads of 64 399, two 440).
+    const int most = std::min(per, std::max(a.t[0].heads, a.t[1].heads));
+    auto start = [&](auto batch) {
+        constexpr int BATCH = decltype(batch)::value;
+        auto kernel = interleaved ? rotate_kernel<T, VP, NU, true, BATCH> : rotate_kernel<T, VP, NU, false, BATCH>;
+        return launch_kernel(kernel, grid, dim3(kRotThreads), 0, stream, a, lanes, per);
+    };
+    if (most == 1) return start(std::integral_constant<int, 1>());
+    if constexpr (VP == 8 && sizeof(T) == 2) {
+        if (most > 5) return start(std::integral_constant<int, 4>());
+    }
+    return start(std::integral_constant<int, 2>());
 }
 
 // Runs of VP elements may be taken together when every address they start at is a multiple of their size.
