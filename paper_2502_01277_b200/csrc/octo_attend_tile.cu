@@ -46,7 +46,9 @@ struct TileShape {
     static constexpr int kQBytes = 2 * kStageBytes;
 };
 
-// What the other roles need to know of an item, left by the loaders.
+// What the other roles need to know of an item, left by the loaders.  The record of item n takes the place of item n - 4's
+// once the queries' place of item n - 1 is free.  A half without rows gives that place back at once, so only its softmax
+// group's last arrival orders the group's read of a record before the writing of the next one in its place.
 struct TileInfo {
     int64_t q0, work;       // first query row of the segment; number of the item
     int kvh, split, row0, rows, last;
@@ -400,6 +402,7 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
             bool look = true;    // the scores have to be looked through before they are weighed
             bool first = true;
             int meta = 0;
+            TileInfo it = {};
             uint32_t s0[32], s1[32], p[32];
             while (!(meta & (kLast | kStop))) {
                 if (!__all_sync(0xffffffffu, tile_wait(&sh->s_full[h][turn & 1], (turn >> 1) & 1, a.status))) {
@@ -490,12 +493,13 @@ attend_tile_kernel(const __grid_constant__ AttendArgs a, int tiles_per_segment, 
                 sum += x + y;
                 tmem_wait_st();
                 tmem_before_sync();
+                // (before the arrival: from there on the record's place may be written again, see TileInfo)
+                if (meta & kLast) it = sh->info[OCTO_TOKEN_IN_RANGE((unsigned)(meta >> kItemShift) < 4u, a.status) ? meta >> kItemShift : 0];
                 mbar_arrive(&sh->p_full[h][turn & 1]);
                 ++turn;
             }
             if (dead || (meta & kStop)) break;
             // the half's rows of the result
-            const TileInfo it = sh->info[OCTO_TOKEN_IN_RANGE((unsigned)(meta >> kItemShift) < 4u, a.status) ? meta >> kItemShift : 0];
             if (!__all_sync(0xffffffffu, tile_wait(&sh->pv_done[h][(turn - 1) & 1], ((turn - 1) >> 1) & 1, a.status))) {
                 dead = true;
                 break;
