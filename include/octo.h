@@ -508,7 +508,8 @@ typedef struct {
  * Norm of every query and key head and its rotation by the token's position, in one pass.
  * For a head x of head_dim elements: y = x * rsqrt(mean(x^2) + eps) * weight (no weight: y = x); then pair i
  * of the first 2 * pairs elements, (i, i + pairs) or with `interleaved` (2 i, 2 i + 1), is turned by the angle
- * position[axis[i]] * freq[i]: (y0 cos - y1 sin, y1 cos + y0 sin); elements from 2 * pairs on stay y.
+ * position[axis[i]] * freq[i]: (y0 cos - y1 sin, y1 cos + y0 sin); elements from 2 * pairs on and pairs of an axis
+ * that is not there stay y, whatever lies beside them.
  * The angle is reduced in 46 bits or more (a position of 2^24 and a frequency of 1 still have a phase that is good
  * to binary32); everything else is binary32, rounded once to the type of the tensors.  For the 16-bit types sine
  * and cosine are off by up to 2^-21.

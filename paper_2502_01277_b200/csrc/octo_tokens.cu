@@ -152,7 +152,8 @@ cudaError_t sm_count_of(int device, int* out) {
 // registers for all heads, multiplied with the norm's weights: a pair (x0, x1) of a head with 1 / rms r becomes
 // r (x0 w0 c - x1 w1 s), r (x1 w1 c + x0 w0 s), six operations.  A lane owns VP pairs of every head, both elements of
 // each: for halves two runs of VP elements that lie `pairs` apart, for neighbours one run of 2 VP, so that no
-// element changes lanes; elements behind the rotated ones are given to lanes as pairs with the angle zero.
+// element changes lanes.  Elements behind the rotated ones are given to lanes as pairs too, but pairs that do not turn are
+// only scaled: as turns by zero an infinity in one element would make its partner NaN (infinity times a sine of zero).
 // ---------------------------------------------------------------------------------------
 struct RotTensor {
     const void* in;
@@ -308,6 +309,7 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lanes, int heads_per_group)
     const int half = a.head_dim / 2, rest = half - a.pairs;  // pairs that turn and do not: `half` in all
     int e0[NU], e1[NU];  // first element of the two runs of a unit (ILV: e1 = e0 + VP)
     bool own[NU];
+    unsigned still = 0;  // bit k: pair k of the lane does not turn
     float cs[N], sn[N];
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
@@ -324,9 +326,11 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lanes, int heads_per_group)
 #pragma unroll
         for (int j = 0; j < VP; ++j) {
             float c = 1.0f, s = 0.0f;
+            still |= 1u << (u * VP + j);
             if (turning) {
                 const int axis = a.axes[p + j];
                 if (axis >= 0 && axis < a.num_axes) {
+                    still &= ~(1u << (u * VP + j));
                     const int64_t at = row * a.num_axes + axis;
                     if (a.positions_are_int) {
                         const int pos = static_cast<const int*>(a.positions)[at];
@@ -342,6 +346,7 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lanes, int heads_per_group)
         }
     }
 
+    const bool some_still = __any_sync(mask, still != 0);
     const float inv_dim = 1.0f / (float)a.head_dim;
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {
@@ -404,27 +409,37 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lanes, int heads_per_group)
                     r[k] = rsqrtf(fmaf(group_sum(sum, mask, first, lanes, in), inv_dim, a.eps));
                 }
             }
+            auto write = [&](auto some) {
+                constexpr bool SOME_STILL = decltype(some)::value;
+                unsigned kept = still;
+                if (SOME_STILL) asm volatile("" : "+r"(kept));  // (else a predicate per pair is kept over the whole loop, and spilled)
 #pragma unroll
-            for (int k = 0; k < BATCH; ++k) {
-                if (h + k >= e) break;
-                T* const head = out_row + (int64_t)(h + k) * t.out_head;
+                for (int k = 0; k < BATCH; ++k) {
+                    if (h + k >= e) break;
+                    T* const head = out_row + (int64_t)(h + k) * t.out_head;
 #pragma unroll
-                for (int u = 0; u < NU; ++u)
-                    if (own[u]) {
-                        float f[2 * VP], y[2 * VP];
-                        run_up<T, VP>(x[k][u][0], f);
-                        run_up<T, VP>(x[k][u][1], f + VP);
+                    for (int u = 0; u < NU; ++u)
+                        if (own[u]) {
+                            float f[2 * VP], y[2 * VP];
+                            run_up<T, VP>(x[k][u][0], f);
+                            run_up<T, VP>(x[k][u][1], f + VP);
 #pragma unroll
-                        for (int j = 0; j < VP; ++j) {
-                            const int m = ILV ? 2 * j : j, n = ILV ? 2 * j + 1 : VP + j, i = u * VP + j;
-                            const float x0 = r[k] * f[m], x1 = r[k] * f[n];
-                            y[m] = fmaf(x0, m00[i], -(x1 * m01[i]));
-                            y[n] = fmaf(x1, m11[i], x0 * m10[i]);
+                            for (int j = 0; j < VP; ++j) {
+                                const int m = ILV ? 2 * j : j, n = ILV ? 2 * j + 1 : VP + j, i = u * VP + j;
+                                const float x0 = r[k] * f[m], x1 = r[k] * f[n];
+                                const bool turns = !SOME_STILL || !((kept >> i) & 1u);
+                                y[m] = fmaf(x0, m00[i], turns ? -(x1 * m01[i]) : -0.0f);
+                                y[n] = fmaf(x1, m11[i], turns ? x0 * m10[i] : -0.0f);
+                            }
+                            *reinterpret_cast<Run<T, VP>*>(head + e0[u]) = run_down<T, VP>(y);
+                            *reinterpret_cast<Run<T, VP>*>(head + e1[u]) = run_down<T, VP>(y + VP);
                         }
-                        *reinterpret_cast<Run<T, VP>*>(head + e0[u]) = run_down<T, VP>(y);
-                        *reinterpret_cast<Run<T, VP>*>(head + e1[u]) = run_down<T, VP>(y + VP);
-                    }
-            }
+                }
+            };
+            // (decided once for the heads in flight; us without the choice, with it here, and with it per head: 274 000 tokens of 16 +
+            // 16 heads of 64, all pairs turning, 393 / 406 / 416; 196 000 tokens of 5 + 5 heads 122 / 129 / 141)
+            if (some_still) write(std::true_type());
+            else write(std::false_type());
         }
     }
 }

@@ -1,10 +1,12 @@
 """Calls of the token operators that their documentation allows and that went wrong, or were held right by time alone, once.
 Tolerances as in test_gpu_tokens."""
+import math
+
 import pytest
 import torch
 
 import paper_2502_01277_b200 as octo
-from test_gpu_tokens import BF16, _attend_ref, _ints, _qkv, _u
+from test_gpu_tokens import BF16, F16, F32, _attend_ref, _gen, _ints, _qkv, _u
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +31,32 @@ def test_attention_tiles_with_and_without_rows_in_their_second_half(dim):
     for _ in range(100):
         assert torch.equal(octo.cross_attention(q, k, v, n, status=status, **kw), first)
     assert int(status) == 0
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("ilv", [False, True])
+@pytest.mark.parametrize("dim,pairs", [(64, 16), (64, 24), (72, 20), (80, 33), (36, 9), (64, 0), (8, 1)])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_an_element_that_does_not_turn_stays_alone(dtype, ilv, dim, pairs, bad):
+    """Elements behind the rotated ones, and pairs of an axis that is not there, are what they were without a norm: an
+    infinity or a NaN among them reaches no other element."""
+    g = _gen(dim + pairs)
+    rows = 6
+    q = torch.randn((rows, 2, dim), generator=g, device="cuda").to(dtype)
+    pos = torch.rand((rows, 1), generator=g, device="cuda") * 9
+    freqs, axes = torch.rand(pairs, generator=g, device="cuda"), torch.zeros(pairs, dtype=torch.int32, device="cuda")
+    if pairs > 2:
+        axes[1], axes[2] = -1, 1
+    still = list(range(2 * pairs, dim))
+    for i in (1, 2) if pairs > 2 else ():
+        still += (2 * i, 2 * i + 1) if ilv else (i, i + pairs)
+    clean, _ = octo.norm_rotate(q, None, pos, freqs, axes, interleaved=ilv)
+    assert torch.equal(clean[..., still], q[..., still])
+    for e in still:
+        x = q.clone()
+        x[1, 0, e] = bad
+        out, _ = octo.norm_rotate(x, None, pos, freqs, axes, interleaved=ilv)
+        want = clean.clone()
+        want[1, 0, e] = bad
+        assert torch.equal(out.nan_to_num(nan=777.0), want.nan_to_num(nan=777.0)), e
+
