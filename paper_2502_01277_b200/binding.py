@@ -388,6 +388,15 @@ def _empty(torch, shape, dtype, device, stream):
     return made
 
 
+def _in_use(stream, *tensors) -> None:
+    """A call on `stream` (None: the current one) reads or writes these tensors: a caller may drop them right after it, and
+    their memory is given out again only when that stream is through."""
+    if stream is not None:
+        for x in tensors:
+            if x is not None:
+                x.record_stream(stream)
+
+
 class Stage:
     """Owns one octo_stage_t and the torch tensors a caller usually wants around it."""
 
@@ -552,6 +561,7 @@ class Stage:
                                                   visible.data_ptr(), self._stream(stream))
         if rc != OCTO_OK:
             raise OctoError(rc, "octo_stage_patch_positions")
+        _in_use(stream, times, positions, visible, self._n_items_keepalive.get(branch))
         return positions, visible
 
     def item_table(self, branch: int, count: int) -> np.ndarray:

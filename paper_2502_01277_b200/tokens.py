@@ -4,8 +4,8 @@ packed crops, norm and rotation of query and key heads, attention to another set
 Argument checks and marshalling only; the work is done by octo_patch_positions, octo_norm_rotate and
 octo_cross_attention of the C ABI (include/octo.h has the rules).  Calls enqueue on the current stream of the
 tensors' device, or on `stream`; nothing synchronises, and a call may be captured into a CUDA graph.  What a call
-allocates belongs to the stream it runs on; inputs have to be ready there.  There is no backward pass: results
-carry no gradient history."""
+allocates belongs to the stream it runs on; inputs have to be ready there, and may be dropped as soon as the call
+returns.  There is no backward pass: results carry no gradient history."""
 from __future__ import annotations
 
 import ctypes
@@ -97,6 +97,7 @@ def patch_positions(items, slot: Tuple[int, int], patch: int, *, keep_aspect: bo
         visible.data_ptr(), _stream_of(dev, stream))
     if rc != B.OCTO_OK:
         raise B.OctoError(rc, "octo_patch_positions")
+    B._in_use(stream, items, times, n_items, positions, visible)
     return positions, visible
 
 
@@ -158,6 +159,7 @@ def norm_rotate(q, k, positions, freqs, axes, *, q_weight=None, k_weight=None, e
     rc = B.load_library().octo_norm_rotate(args, _stream_of(dev, stream))
     if rc != B.OCTO_OK:
         raise B.OctoError(rc, "octo_norm_rotate")
+    B._in_use(stream, q, k, positions, freqs, axes, q_weight, k_weight, n_items, q_out, k_out)
     return q_out, k_out
 
 
@@ -219,4 +221,5 @@ def cross_attention(q, k, v, segments: int, *, q_offsets=None, k_offsets=None, q
     rc = lib.octo_cross_attention(args, None if workspace is None else workspace.data_ptr(), need.value, _stream_of(dev, stream))
     if rc != B.OCTO_OK:
         raise B.OctoError(rc, "octo_cross_attention")
+    B._in_use(stream, q, k, v, q_offsets, k_offsets, key_mask, out, status)
     return out

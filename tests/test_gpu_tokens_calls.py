@@ -60,3 +60,108 @@ def test_an_element_that_does_not_turn_stays_alone(dtype, ilv, dim, pairs, bad):
         want[1, 0, e] = bad
         assert torch.equal(out.nan_to_num(nan=777.0), want.nan_to_num(nan=777.0)), e
 
+
+@pytest.mark.parametrize("which", ["attention", "rotation", "positions", "stage"])
+def test_inputs_of_a_call_on_another_stream_may_be_let_go_of(which):
+    """What a call on a given stream reads stays what it is until that stream has read it, although the caller drops
+    it and the current stream hands its memory out again."""
+    g = _gen(21)
+    q, k, v = _qkv(21, 40, 900, 4, 2, 64, BF16)
+    pos = torch.rand((40, 1), generator=g, device="cuda") * 100
+    freqs, axes = torch.rand(32, generator=g, device="cuda"), torch.zeros(32, dtype=torch.int32, device="cuda")
+    mask = (torch.rand(900, generator=g, device="cuda") < 0.5).to(torch.uint8)
+    weight = torch.rand(64, generator=g, device="cuda").to(BF16)
+    items = torch.zeros((64, 8), dtype=torch.int32, device="cuda")
+    items[:, 4:6] = 100
+    times = torch.rand(1, generator=g, device="cuda")
+    st = None
+    if which == "attention":
+        given = [q, k, v, _ints([0, 3, 10]), _ints([0, 400, 900]), mask]
+        call = lambda s, q, k, v, qo, ko, m: (octo.cross_attention(q, k, v, 2, q_offsets=qo, k_offsets=ko, q_rows=4, key_mask=m,
+                                                                   stream=s),)
+    elif which == "rotation":
+        given = [q, k[:40], pos, freqs, axes, weight, weight + 1, _ints([40])]
+        call = lambda s, q, k, p, f, a, w, x, n: octo.norm_rotate(q, k, p, f, a, q_weight=w, k_weight=x, n_items=n, stream=s)
+    elif which == "positions":
+        given = [items, times, _ints([64])]
+        call = lambda s, i, t, n: octo.patch_positions(i, (224, 224), 16, times=t, n_items=n, stream=s)
+    else:
+        import workloads
+        from gpu_harness import make_stage, upload_frames
+        b = workloads.make_batch("two_branch", batch=3)
+        st = make_stage(b.workload, b.n)
+        frames, head = upload_frames(b.frames), torch.from_numpy(b.head).cuda()
+        st.preprocess(frames, b.sizes)
+        st.postprocess(head)
+        _, _, count = st.crop(0, 8)
+        assert int(count[0]) == 8
+        given = [torch.tensor([3.0, 4.0, 5.0], device="cuda")]
+        call = lambda s, t: st.patch_positions(0, 8, 16, times=t, stream=s)
+    want = [w.clone() for w in call(None, *given)]
+    side = torch.cuda.Stream()
+    for n in range(len(given)):
+        args = [x.clone() if i == n else x for i, x in enumerate(given)]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)
+        got = call(side, *args)
+        args[n] = None
+        again = [torch.empty_like(given[n]) for _ in range(64)]  # (many small blocks may be free)
+        for x in again:
+            x.fill_(77 if x.dtype in (torch.int32, torch.uint8) else 1e4)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), n
+        del again
+    if st is not None:
+        st.close()
+
+
+def test_an_output_of_a_call_on_another_stream_may_be_let_go_of():
+    """A result that the caller drops is written by the given stream before its memory is anyone else's."""
+    q, k, v = _qkv(22, 64, 900, 4, 2, 64, BF16)
+    side = torch.cuda.Stream()
+    for use in (lambda o: octo.cross_attention(q, k, v, 1, q_rows=64, k_rows=900, out=o, stream=side),
+                lambda o: octo.norm_rotate(q, None, torch.zeros((64, 1), device="cuda"), torch.zeros(32, device="cuda"),
+                                           torch.zeros(32, dtype=torch.int32, device="cuda"), out=(o, None), stream=side)):
+        out = torch.empty_like(q)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)
+        use(out)
+        del out
+        again = [torch.empty_like(q).fill_(5.0) for _ in range(4)]
+        torch.cuda.synchronize()
+        assert all((x == 5.0).all() for x in again)
+        del again
+
+
+def test_calls_on_a_forked_stream_inside_a_capture():
+    """The same inside a CUDA graph: temporaries of the capturing stream, read on a stream forked from it."""
+    q, k, v = _qkv(24, 64, 20000, 4, 2, 64, BF16)
+    pos, freqs = torch.rand((64, 1), device="cuda") * 100, torch.rand(32, device="cuda")
+    axes = torch.zeros(32, dtype=torch.int32, device="cuda")
+
+    def one_pass(side):
+        main = torch.cuda.current_stream()
+        turned, _ = octo.norm_rotate(q + q, None, pos, freqs, axes)
+        kk, vv = k + k, v + v  # (ready on the other stream: before it waits for this one)
+        if side is not None:
+            side.wait_stream(main)
+        out = octo.cross_attention(turned, kk, vv, 1, q_rows=64, k_rows=20000, stream=side)
+        del turned, kk, vv
+        if side is not None:
+            main.wait_stream(side)
+        return out
+
+    want = one_pass(None)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = one_pass(side)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    del graph, out
+    assert torch.equal(one_pass(side), want)
