@@ -529,7 +529,9 @@ extern "C" int octo_cross_attention(const octo_attend_t* c, void* d_workspace, i
     a.max_k = bound_of(c->max_k, c->d_k_offsets, c->k_rows, c->k_total);
     a.mask = c->d_key_mask;
     a.scale_log2 = (float)((double)c->scale * 1.44269504088896340736);
-    if (a.scale_log2 == 0.0f) a.scale_log2 = 1e-30f;  // equal weights, and still no weight for what is hidden (-infinity)
+    // Equal weights, and still no weight for what is hidden (-infinity): the smallest number there is, 1.4e-45, makes of any
+    // finite score at most 2^-21.
+    if (a.scale_log2 == 0.0f) a.scale_log2 = 1e-45f;
     a.segments = c->segments;
     a.heads = c->heads;
     a.kv_heads = c->kv_heads;

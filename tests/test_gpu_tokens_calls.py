@@ -165,3 +165,13 @@ def test_calls_on_a_forked_stream_inside_a_capture():
         assert torch.equal(out, want)
     del graph, out
     assert torch.equal(one_pass(side), want)
+
+
+@pytest.mark.parametrize("q_rows", [1, 6000])
+def test_attention_scale_zero_is_the_mean_whatever_the_scores(q_rows):
+    """Scores up to 2^125."""
+    q, k, v = _qkv(23, q_rows, 1500, 2, 2, 64, BF16)
+    q, k = torch.sign(q) * 2.0**60, torch.sign(k) * 2.0**59
+    out = octo.cross_attention(q, k, v, 1, q_rows=q_rows, k_rows=1500, scale=0.0)
+    want, size = v.double().mean(0), v.double().abs().mean(0)
+    assert ((out.double() - want).abs() <= (2 * _u(BF16) + 2.0**-15) * size).all()
