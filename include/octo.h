@@ -468,6 +468,7 @@ OCTO_API int octo_static_status(int32_t device, uint32_t* status_word, void* cud
 
 /*
  * Where the patches of packed crops lie in time and in their source frames.
+ *   max_items  0 .. 2^30.
  *   d_items    device, [max_items] records of an item table (octo_stage_item_table, or records that the
  *              caller wrote: the letterboxed canvas of a frame is an item whose rectangle is the whole
  *              frame, with keep_aspect = 1).  4-byte aligned.

@@ -514,7 +514,7 @@ extern "C" int octo_patch_positions(int32_t device, const octo_item_t* d_items, 
                                     int32_t slot_w, int32_t slot_h, int32_t patch, int32_t keep_aspect,
                                     const float* d_times, int32_t n_frames, float* d_positions, uint8_t* d_visible,
                                     void* cuda_stream) {
-    if (device < 0 || max_items < 0 || n_frames < 0) return OCTO_E_INVALID_ARG;
+    if (device < 0 || max_items < 0 || max_items > 1 << 30 || n_frames < 0) return OCTO_E_INVALID_ARG;
     if (slot_w < 1 || slot_w > kPosMaxSide || slot_h < 1 || slot_h > kPosMaxSide || patch < 1) return OCTO_E_INVALID_ARG;
     if (slot_w % patch || slot_h % patch || (keep_aspect != 0 && keep_aspect != 1)) return OCTO_E_INVALID_ARG;
     if (max_items == 0) return OCTO_OK;

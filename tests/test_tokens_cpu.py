@@ -153,3 +153,9 @@ def test_attention_refuses_rows_that_32_bits_cannot_number(lib, heads, kv_heads,
     need = ctypes.c_int64(7)
     rc = lib.octo_attend_workspace(ctypes.byref(_attend(heads=heads, kv_heads=kv_heads, q_total=q_total)), ctypes.byref(need))
     assert (rc != B.OCTO_E_CAPACITY) == fits and need.value == 0
+
+
+@pytest.mark.parametrize("items", [(1 << 30) + 1, (1 << 31) - 1])
+def test_positions_refuses_more_items_than_its_grid_numbers(lib, items):
+    """Items are numbered in 32 bits, up to a CTA's more than there are."""
+    assert _positions(lib, max_items=items) == B.OCTO_E_INVALID_ARG
