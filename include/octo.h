@@ -499,7 +499,8 @@ OCTO_API int octo_stage_patch_positions(octo_stage_t* st, int32_t branch, int32_
                                         const float* d_times, float* d_positions, uint8_t* d_visible,
                                         void* cuda_stream);
 
-/* One tensor [rows, heads, head_dim] of a token call; the elements of a head lie side by side. */
+/* One tensor [rows, heads, head_dim] of a token call; the elements of a head lie side by side.  Rows or heads of an
+ * input may lie on one another (a stride of 0), those of an output may not: such strides are refused. */
 typedef struct {
     void* d_data;
     int64_t row_stride, head_stride; /* elements */

@@ -24,6 +24,10 @@ struct DeviceScope {
 };
 
 inline bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+// An output whose rows or heads lie on one another (an expanded tensor): which of them stayed would be a matter of time.
+inline bool rows_coincide(const octo_heads_t& t, int64_t rows, int heads) {
+    return rows > 0 && heads > 0 && ((t.row_stride == 0 && rows > 1) || (t.head_stride == 0 && heads > 1));
+}
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // Division by a number that is the same for a whole launch: exact for 0 <= n < 2^31 (multiply by the reciprocal rounded

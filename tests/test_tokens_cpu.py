@@ -159,3 +159,22 @@ def test_attention_refuses_rows_that_32_bits_cannot_number(lib, heads, kv_heads,
 def test_positions_refuses_more_items_than_its_grid_numbers(lib, items):
     """Items are numbered in 32 bits, up to a CTA's more than there are."""
     assert _positions(lib, max_items=items) == B.OCTO_E_INVALID_ARG
+
+
+@pytest.mark.parametrize("over", [{"out.row_stride": 0}, {"out.head_stride": 0}])
+def test_attention_refuses_an_output_whose_rows_or_heads_coincide(lib, over):
+    assert lib.octo_cross_attention(ctypes.byref(_attend(**over)), None, 0, None) == B.OCTO_E_INVALID_ARG
+
+
+@pytest.mark.parametrize("over", [{"q_out.row_stride": 0}, {"q_out.head_stride": 0}, {"k_out.row_stride": 0}, {"k_out.head_stride": 0}])
+def test_rotation_refuses_an_output_whose_rows_or_heads_coincide(lib, over):
+    assert lib.octo_norm_rotate(ctypes.byref(_rotate(**over)), None) == B.OCTO_E_INVALID_ARG
+
+
+def test_strides_of_one_row_or_head_mean_nothing(lib):
+    """(Where they are accepted the call goes on to the device, which is missing here or takes a call without work.)"""
+    one = {"q_total": 1, "heads": 1, "kv_heads": 1, "out.row_stride": 0, "out.head_stride": 0, "device": 1 << 20}
+    assert lib.octo_cross_attention(ctypes.byref(_attend(**one)), None, 0, None) == B.OCTO_E_CUDA
+    one = {"rows": 1, "heads": 1, "kv_heads": 1, "q_out.row_stride": 0, "q_out.head_stride": 0, "k_out.row_stride": 0,
+           "k_out.head_stride": 0, "device": 1 << 20}
+    assert lib.octo_norm_rotate(ctypes.byref(_rotate(**one)), None) == B.OCTO_E_CUDA
