@@ -571,7 +571,8 @@ typedef struct {
     float scale;                      /* magnitude at most 1e30                                            */
     float _pad;
     uint32_t* d_status;               /* one word, or NULL: OCTO_STATUS_COPY_TIMEOUT is set (and the rows  */
-                                      /* concerned become NaN) if a bounded wait of the kernel gives up    */
+                                      /* concerned become NaN) if a bounded wait of the kernel gives up,   */
+                                      /* after 17 s or more                                                */
 } octo_attend_t;
 
 #define OCTO_MAX_SEGMENTS 2048

@@ -212,10 +212,13 @@ __device__ __forceinline__ void tile_row(const AttendArgs& a, int kvh, int r, in
     head = kvh * a.group + (r - qrow * a.group);
 }
 
-// One wait of a role.  A wait that runs out is reported; the role then leaves, and so do the others in turn.
+// One wait of a role.  A wait that runs out is reported; the role then leaves, and so do the others in turn.  2^23 polls are 17 s
+// or more.  What takes longest in a call that works is looking through hidden keys: 5 s for the 2^30 that there can be,
+// during which all other roles wait.  (Asking the loaders for signs of life instead cost 5 % of every call.)
+constexpr int kTilePolls = 1 << 23;
 __device__ __forceinline__ bool tile_wait(uint64_t* bar, uint32_t parity, unsigned int* status) {
 #pragma unroll 1  // (the loops of five roles were a third of the kernel's code)
-    for (int i = 0; i < 1 << 20; ++i)
+    for (int i = 0; i < kTilePolls; ++i)
         if (mbar_try_wait(bar, parity)) return true;
     if (status) atomicOr(status, OCTO_STATUS_COPY_TIMEOUT);
     return false;

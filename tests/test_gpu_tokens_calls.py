@@ -175,3 +175,23 @@ def test_attention_scale_zero_is_the_mean_whatever_the_scores(q_rows):
     out = octo.cross_attention(q, k, v, 1, q_rows=q_rows, k_rows=1500, scale=0.0)
     want, size = v.double().mean(0), v.double().abs().mean(0)
     assert ((out.double() - want).abs() <= (2 * _u(BF16) + 2.0**-15) * size).all()
+
+
+def test_attention_looks_through_a_billion_hidden_keys():
+    """One segment of 2^30 - 1196 keys, all hidden, which takes seconds to look through, beside 299 of four keys: waiting that
+    long is not a wait that has run out.  (The keys are one row in memory, seen again and again.)"""
+    n, q_rows, dim = 300, 32, 8
+    first = (1 << 30) - 4 * (n - 1)
+    g = _gen(25)
+    q = torch.randn((n * q_rows, 1, dim), generator=g, device="cuda").to(BF16)
+    k, v = (torch.randn((1, 1, dim), generator=g, device="cuda").to(BF16).expand(1 << 30, 1, dim) for _ in range(2))
+    mask = torch.zeros(1 << 30, dtype=torch.uint8, device="cuda")
+    mask[first:] = 1
+    offsets = _ints([0] + [first + 4 * i for i in range(n)])
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = octo.cross_attention(q, k, v, n, q_rows=q_rows, k_offsets=offsets, key_mask=mask, status=status)
+    assert int(status) == 0
+    assert (out[:q_rows] == 0).all()
+    assert ((out[q_rows:].double() - v[:1].double()).abs() <= (2 * _u(BF16) + 2.0**-15) * v[:1].double().abs()).all()
+    del mask
+    torch.cuda.empty_cache()
