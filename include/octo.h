@@ -540,6 +540,10 @@ typedef struct {
 /* Errors: OCTO_E_INVALID_ARG, OCTO_E_ALIGNMENT (a pointer not a multiple of its element's size), OCTO_E_CUDA. */
 OCTO_API int octo_norm_rotate(const octo_rotate_t* args, void* cuda_stream);
 
+/* How a call with these arguments is carried out: elements that are loaded in a row, heads that a warp walks over and
+ * heads it has in flight.  Enqueues nothing.  Errors as octo_norm_rotate; zeros for a call without rows. */
+OCTO_API int octo_rotate_plan(const octo_rotate_t* args, int32_t* run, int32_t* heads_per_warp, int32_t* heads_in_flight);
+
 /*
  * Attention of one set of tokens to another set's states, segment by segment.
  * Segment s has the query rows [q0, q1) and the key rows [k0, k1), where q0 = (b - q_first) * q_rows with
@@ -580,6 +584,11 @@ typedef struct {
 /* Bytes of workspace that octo_cross_attention needs for these arguments (of the pointers it only matters which
  * offsets are NULL); 0 where no work is split over the keys. */
 OCTO_API int octo_attend_workspace(const octo_attend_t* args, int64_t* bytes);
+
+/* How a call with these arguments is carried out: 1 in *tile for the kernel for many query rows, 0 for the one for few;
+ * the number of parts that the keys are split into.  Enqueues nothing.  Errors as octo_attend_workspace; 0 and 0 for a
+ * call without rows. */
+OCTO_API int octo_attend_plan(const octo_attend_t* args, int32_t* tile, int32_t* splits);
 
 /* d_workspace: device, at least that many bytes, 16-byte aligned; its contents mean nothing between calls.
  * Errors: OCTO_E_INVALID_ARG, OCTO_E_CAPACITY (too many segments, a workspace that is too small),

@@ -59,7 +59,7 @@ EXPORTS = (
     "octo_adopt_items_device", "octo_stage_selftest_wait", "octo_static_status",
     "octo_stage_set_nms_cluster", "octo_stage_last_nms_cluster", "octo_stage_last_nms_half_ctas",
     "octo_patch_positions", "octo_stage_patch_positions", "octo_norm_rotate", "octo_attend_workspace",
-    "octo_cross_attention",
+    "octo_cross_attention", "octo_rotate_plan", "octo_attend_plan",
 )
 
 
@@ -232,8 +232,10 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.octo_norm_rotate.argtypes = [vp, vp]  # (octo_rotate_t packed into bytes, or by reference)
     lib.octo_attend_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_int64)]
     lib.octo_cross_attention.argtypes = [vp, vp, ctypes.c_int64, vp]
+    lib.octo_rotate_plan.argtypes = [vp] + [ctypes.POINTER(i32)] * 3
+    lib.octo_attend_plan.argtypes = [vp] + [ctypes.POINTER(i32)] * 2
     for name in ("octo_patch_positions", "octo_stage_patch_positions", "octo_norm_rotate", "octo_attend_workspace",
-                 "octo_cross_attention"):
+                 "octo_cross_attention", "octo_rotate_plan", "octo_attend_plan"):
         getattr(lib, name).restype = ctypes.c_int
     lib.octo_coral_schedule.argtypes = [ctypes.POINTER(CoralInstance), i32, ctypes.POINTER(CoralGpu), i32,
                                         ctypes.POINTER(CoralPlacement)]

@@ -466,19 +466,39 @@ static cudaError_t launch_attend(const AttendArgs& a, const AttendPlan& p, cudaS
 
 using namespace octo;
 
+// The plan of a call; `work` says whether there is any.
+static int plan_of(const octo_attend_t* c, AttendPlan* p, bool* work, const char* where) {
+    *work = false;
+    const int rc = validate(c);
+    if (rc != OCTO_OK || c->q_total == 0) return rc;
+    int sms = 0;
+    const cudaError_t e = sm_count_of(c->device, &sms);
+    if (e != cudaSuccess) return report_cuda_error(e, where);
+    *work = true;
+    return make_plan(c, sms, p);
+}
+
 extern "C" int octo_attend_workspace(const octo_attend_t* c, int64_t* bytes) {
     if (!bytes) return OCTO_E_INVALID_ARG;
     *bytes = 0;
-    const int rc = validate(c);
-    if (rc != OCTO_OK) return rc;
-    if (c->q_total == 0) return OCTO_OK;
-    int sms = 0;
-    const cudaError_t e = sm_count_of(c->device, &sms);
-    if (e != cudaSuccess) return report_cuda_error(e, "octo_attend_workspace");
     AttendPlan p;
-    const int prc = make_plan(c, sms, &p);
-    if (prc == OCTO_OK) *bytes = p.workspace;
-    return prc;
+    bool work;
+    const int rc = plan_of(c, &p, &work, "octo_attend_workspace");
+    if (rc == OCTO_OK && work) *bytes = p.workspace;
+    return rc;
+}
+
+extern "C" int octo_attend_plan(const octo_attend_t* c, int32_t* tile, int32_t* splits) {
+    if (!tile || !splits) return OCTO_E_INVALID_ARG;
+    *tile = *splits = 0;
+    AttendPlan p;
+    bool work;
+    const int rc = plan_of(c, &p, &work, "octo_attend_plan");
+    if (rc == OCTO_OK && work) {
+        *tile = p.tile ? 1 : 0;
+        *splits = p.splits;
+    }
+    return rc;
 }
 
 extern "C" int octo_cross_attention(const octo_attend_t* c, void* d_workspace, int64_t workspace_bytes, void* cuda_stream) {

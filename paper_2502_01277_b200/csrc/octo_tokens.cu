@@ -444,8 +444,14 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lanes, int heads_per_group)
     }
 }
 
+// How a call is carried out (octo_rotate_plan).
+struct RotateForm {
+    int run, per, in_flight;
+};
+
+// Launches, or with `form` only says how it would.
 template <typename T, int VP, int NU>
-static cudaError_t launch_rotate(const RotArgs& a, bool interleaved, int sm_count, cudaStream_t stream) {
+static cudaError_t launch_rotate(const RotArgs& a, bool interleaved, int sm_count, cudaStream_t stream, RotateForm* form) {
     const int lanes = ceil_div(ceil_div(a.head_dim / 2, VP), NU), tokens = 32 / lanes;
     const int total = a.t[0].heads + a.t[1].heads;
     const int64_t warps = (a.rows + tokens - 1) / tokens;
@@ -466,6 +472,10 @@ static cudaError_t launch_rotate(const RotArgs& a, bool interleaved, int sm_coun
     const int most = std::min(per, std::max(a.t[0].heads, a.t[1].heads));
     auto start = [&](auto batch) {
         constexpr int BATCH = decltype(batch)::value;
+        if (form) {
+            *form = {VP, per, BATCH};
+            return cudaSuccess;
+        }
         auto kernel = interleaved ? rotate_kernel<T, VP, NU, true, BATCH> : rotate_kernel<T, VP, NU, false, BATCH>;
         return launch_kernel(kernel, grid, dim3(kRotThreads), 0, stream, a, lanes, per);
     };
@@ -492,18 +502,19 @@ static bool runs_of(const octo_rotate_t& c, const RotArgs& a, int vp, int esize)
 }
 
 template <typename T>
-static cudaError_t rotate_typed(const octo_rotate_t& c, const RotArgs& a, int sm_count, cudaStream_t stream) {
-    if (runs_of(c, a, 8, (int)sizeof(T))) return launch_rotate<T, 8, 1>(a, c.interleaved != 0, sm_count, stream);
-    if (runs_of(c, a, 4, (int)sizeof(T))) return launch_rotate<T, 4, 1>(a, c.interleaved != 0, sm_count, stream);
+static cudaError_t rotate_typed(const octo_rotate_t& c, const RotArgs& a, int sm_count, cudaStream_t stream, RotateForm* form) {
+    if (runs_of(c, a, 8, (int)sizeof(T))) return launch_rotate<T, 8, 1>(a, c.interleaved != 0, sm_count, stream, form);
+    if (runs_of(c, a, 4, (int)sizeof(T))) return launch_rotate<T, 4, 1>(a, c.interleaved != 0, sm_count, stream, form);
     // Shorter runs: two units per lane where a warp then takes two tokens rather than one (one fp32 head of 72 with 18
     // turning pairs in q and k, 835 000 tokens: 1070 us with one unit, 620 with two).
     const int half = c.head_dim / 2;
     const bool ilv = c.interleaved != 0;
     if (runs_of(c, a, 2, (int)sizeof(T)))
-        return half <= 32 ? launch_rotate<T, 2, 1>(a, ilv, sm_count, stream) : launch_rotate<T, 2, 2>(a, ilv, sm_count, stream);
-    if (half <= 16) return launch_rotate<T, 1, 1>(a, ilv, sm_count, stream);
-    if (half <= 32) return launch_rotate<T, 1, 2>(a, ilv, sm_count, stream);
-    return launch_rotate<T, 1, 4>(a, ilv, sm_count, stream);
+        return half <= 32 ? launch_rotate<T, 2, 1>(a, ilv, sm_count, stream, form)
+                          : launch_rotate<T, 2, 2>(a, ilv, sm_count, stream, form);
+    if (half <= 16) return launch_rotate<T, 1, 1>(a, ilv, sm_count, stream, form);
+    if (half <= 32) return launch_rotate<T, 1, 2>(a, ilv, sm_count, stream, form);
+    return launch_rotate<T, 1, 4>(a, ilv, sm_count, stream, form);
 }
 
 }  // namespace octo
@@ -531,7 +542,7 @@ extern "C" int octo_patch_positions(int32_t device, const octo_item_t* d_items, 
     return e == cudaSuccess ? OCTO_OK : report_cuda_error(e, "octo_patch_positions");
 }
 
-extern "C" int octo_norm_rotate(const octo_rotate_t* c, void* cuda_stream) {
+static int rotate_call(const octo_rotate_t* c, void* cuda_stream, RotateForm* form) {
     if (!c || c->device < 0) return OCTO_E_INVALID_ARG;
     if (c->dtype != OCTO_F16 && c->dtype != OCTO_BF16 && c->dtype != OCTO_F32) return OCTO_E_INVALID_ARG;
     if (c->heads < 0 || c->kv_heads < 0 || c->heads > 16384 || c->kv_heads > 16384 || c->heads + c->kv_heads < 1)
@@ -577,9 +588,21 @@ extern "C" int octo_norm_rotate(const octo_rotate_t* c, void* cuda_stream) {
     cudaError_t e = sm_count_of(c->device, &sms);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (e == cudaSuccess) {
-        if (c->dtype == OCTO_F16) e = rotate_typed<__half>(*c, a, sms, stream);
-        else if (c->dtype == OCTO_BF16) e = rotate_typed<__nv_bfloat16>(*c, a, sms, stream);
-        else e = rotate_typed<float>(*c, a, sms, stream);
+        if (c->dtype == OCTO_F16) e = rotate_typed<__half>(*c, a, sms, stream, form);
+        else if (c->dtype == OCTO_BF16) e = rotate_typed<__nv_bfloat16>(*c, a, sms, stream, form);
+        else e = rotate_typed<float>(*c, a, sms, stream, form);
     }
     return e == cudaSuccess ? OCTO_OK : report_cuda_error(e, "octo_norm_rotate");
+}
+
+extern "C" int octo_norm_rotate(const octo_rotate_t* c, void* cuda_stream) { return rotate_call(c, cuda_stream, nullptr); }
+
+extern "C" int octo_rotate_plan(const octo_rotate_t* c, int32_t* run, int32_t* heads_per_warp, int32_t* heads_in_flight) {
+    if (!run || !heads_per_warp || !heads_in_flight) return OCTO_E_INVALID_ARG;
+    RotateForm form = {0, 0, 0};
+    const int rc = rotate_call(c, nullptr, &form);
+    *run = form.run;
+    *heads_per_warp = form.per;
+    *heads_in_flight = form.in_flight;
+    return rc;
 }

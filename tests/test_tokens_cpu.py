@@ -178,3 +178,23 @@ def test_strides_of_one_row_or_head_mean_nothing(lib):
     one = {"rows": 1, "heads": 1, "kv_heads": 1, "q_out.row_stride": 0, "q_out.head_stride": 0, "k_out.row_stride": 0,
            "k_out.head_stride": 0, "device": 1 << 20}
     assert lib.octo_norm_rotate(ctypes.byref(_rotate(**one)), None) == B.OCTO_E_CUDA
+
+
+@pytest.mark.parametrize("over,code", BAD_ATTEND)
+def test_attention_plan_refuses_what_the_call_refuses(lib, over, code):
+    tile, splits = ctypes.c_int32(7), ctypes.c_int32(7)
+    assert lib.octo_attend_plan(ctypes.byref(_attend(**over)), ctypes.byref(tile), ctypes.byref(splits)) == code
+    assert (tile.value, splits.value) == (0, 0)
+
+
+def test_plans_null_and_empty(lib):
+    a, b, c = (ctypes.c_int32(7) for _ in range(3))
+    refs = [ctypes.byref(x) for x in (a, b, c)]
+    assert lib.octo_attend_plan(None, *refs[:2]) == B.OCTO_E_INVALID_ARG
+    assert lib.octo_attend_plan(ctypes.byref(_attend()), None, refs[0]) == B.OCTO_E_INVALID_ARG
+    assert lib.octo_attend_plan(ctypes.byref(_attend(q_total=0)), *refs[:2]) == B.OCTO_OK and a.value == b.value == 0
+    assert lib.octo_rotate_plan(None, *refs) == B.OCTO_E_INVALID_ARG
+    assert lib.octo_rotate_plan(ctypes.byref(_rotate()), None, None, None) == B.OCTO_E_INVALID_ARG
+    assert lib.octo_rotate_plan(ctypes.byref(_rotate(head_dim=63)), *refs) == B.OCTO_E_INVALID_ARG
+    a.value = b.value = c.value = 7
+    assert lib.octo_rotate_plan(ctypes.byref(_rotate(rows=0)), *refs) == B.OCTO_OK and a.value == b.value == c.value == 0
