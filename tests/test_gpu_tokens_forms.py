@@ -194,3 +194,70 @@ def test_crops_of_a_stage_in_tiles(forms):
     k, v = (torch.randn((b.n * states, 2, 64), generator=g, device="cuda").to(BF16) for _ in range(2))
     _tile_check(forms, q, k, v, b.n, q_offsets=offsets, q_rows=tokens, k_rows=states, q_first=first)
     st.close()
+
+
+# ---- norm and rotation: heads in flight -----------------------------------------------------------------------------
+
+def _rotate_case(rows, heads, kv, dim, pairs, dtype, seed):
+    g = _gen(seed)
+    qkv = torch.randn((rows, heads + kv, dim), generator=g, device="cuda").to(dtype)
+    pos = torch.rand((rows, 3), generator=g, device="cuda") * torch.tensor([16777216.0, 1080.0, 1.0], device="cuda")
+    freqs = torch.rand(pairs, generator=g, device="cuda") * 2
+    axes = torch.randint(0, 3, (pairs,), generator=g, device="cuda").int()
+    if pairs > 8:
+        axes[1], axes[3] = -1, 3  # no axis of these numbers: the pairs stay
+    w = (1 + 0.3 * torch.randn(dim, generator=g, device="cuda")).to(dtype)
+    x = (1 + 0.3 * torch.randn(dim, generator=g, device="cuda")).to(dtype)
+    return qkv, pos, freqs, axes, w, x
+
+
+# (heads, kv, dim, pairs): all heads of a token in one warp, in flight one, two or four; the last group of heads not full
+# in some; queries and keys of one warp under weights of their own
+MANY = [(F16, 16, 16, 64, 32, 8, 4), (BF16, 7, 3, 64, 32, 8, 4), (F16, 6, 1, 128, 32, 8, 4), (F16, 5, 5, 64, 32, 8, 2),
+        (BF16, 4, 3, 96, 24, 8, 2), (F16, 1, 1, 64, 32, 8, 1), (F16, 7, 3, 72, 36, 4, 2), (BF16, 3, 2, 254, 127, 1, 2),
+        (F16, 1, 1, 254, 100, 1, 1), (F32, 16, 16, 64, 32, 8, 2), (F32, 7, 3, 72, 24, 4, 2), (F32, 1, 1, 72, 18, 2, 1),
+        (F32, 5, 5, 64, 16, 8, 2), (BF16, 9, 2, 20, 10, 2, 2), (F16, 6, 3, 36, 9, 1, 2)]
+
+
+@pytest.mark.parametrize("dtype,heads,kv,dim,pairs,run,flight", MANY)
+@pytest.mark.parametrize("ilv", [False, True])
+@pytest.mark.parametrize("weights", ["q", "k", "both", "none"])
+def test_rotation_of_many_tokens(forms, dtype, heads, kv, dim, pairs, run, flight, ilv, weights):
+    rows = 20011
+    qkv, pos, freqs, axes, w, x = _rotate_case(rows, heads, kv, dim, pairs, dtype, dim + heads)
+    q, k = qkv[:, :heads], qkv[:, heads:]
+    wq, wk = (w if weights in ("q", "both") else None), (x if weights in ("k", "both") else None)
+    qo, ko = octo.norm_rotate(q, k, pos, freqs, axes, q_weight=wq, k_weight=wk, eps=1e-5, interleaved=ilv)
+    got_run, per, got_flight = forms.seen[-1]
+    assert per == heads + kv and got_flight == flight and (ilv or got_run == run)
+    for got, a, b in ((qo, q, wq), (ko, k, wk)):
+        want, size = _rotate_ref(a, b, pos, freqs, axes, 1e-5, ilv)
+        _rotate_check(got, want, size, dtype)
+    if weights == "both":  # in place, and rows that no item fills
+        n = _ints([2001])
+        before = qkv.clone()
+        octo.norm_rotate(q, k, pos, freqs, axes, q_weight=wq, k_weight=wk, eps=1e-5, interleaved=ilv, n_items=n, item_rows=7,
+                         out=(q, k))
+        assert torch.equal(q[:14007], qo[:14007]) and torch.equal(k[:14007], ko[:14007])
+        assert torch.equal(qkv[14007:], before[14007:])
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("heads,kv,dim,pairs", [(16, 16, 64, 32), (13, 6, 64, 32), (7, 5, 72, 24), (9, 0, 128, 64), (11, 4, 254, 127)])
+@pytest.mark.parametrize("ilv", [False, True])
+def test_rotation_with_the_heads_of_a_token_on_several_warps(forms, dtype, heads, kv, dim, pairs, ilv):
+    """More than one head a warp and fewer than all: groups that lie over the border of queries and keys, and a last group
+    that is not full."""
+    seen = set()
+    for rows in (300, 700, 1500, 4000, 9000, 15000):
+        qkv, pos, freqs, axes, w, x = _rotate_case(rows, heads, kv, dim, pairs, dtype, rows)
+        q, k = qkv[:, :heads], qkv[:, heads:] if kv else None
+        qo, ko = octo.norm_rotate(q, k, pos, freqs, axes, q_weight=w, k_weight=x if kv else None, eps=1e-5, interleaved=ilv)
+        if not 1 < forms.seen[-1][1] < heads + kv:
+            continue
+        seen.add(forms.seen[-1][1])
+        for got, a, b in ((qo, q, w), (ko, k, x)):
+            if a is not None:
+                want, size = _rotate_ref(a, b, pos, freqs, axes, 1e-5, ilv)
+                _rotate_check(got, want, size, dtype)
+    assert seen, "no call had several heads on a warp and not all"
