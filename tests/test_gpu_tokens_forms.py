@@ -261,3 +261,81 @@ def test_rotation_with_the_heads_of_a_token_on_several_warps(forms, dtype, heads
                 want, size = _rotate_ref(a, b, pos, freqs, axes, 1e-5, ilv)
                 _rotate_check(got, want, size, dtype)
     assert seen, "no call had several heads on a warp and not all"
+
+
+# ---- positions: a warp or a CTA per item ----------------------------------------------------------------------------
+
+def _fits(rec, slot, keep):
+    """Size and place of the images, in whole numbers."""
+    ow, oh = slot
+    cw, ch = (rec[:, 4] - rec[:, 2]).astype(object), (rec[:, 5] - rec[:, 3]).astype(object)
+    out = []
+    for w, h in zip(cw, ch):
+        nw, nh = ow, oh
+        if keep and w > 0 and h > 0:
+            if ow * h <= oh * w:
+                nh = max(1, (2 * ow * h + w) // (2 * w))
+            else:
+                nw = max(1, (2 * oh * w + h) // (2 * h))
+        out.append((nw, nh, (ow - nw) // 2, (oh - nh) // 2))
+    return np.array(out, dtype=np.int64)
+
+
+def _places(rec, slot, p, keep, times):
+    """Positions in 64 bits and visibility of all items' patches."""
+    rec = rec.astype(np.int64)
+    gw, gh = slot[0] // p, slot[1] // p
+    fit = _fits(rec, slot, keep)
+    good = (rec[:, 4] > rec[:, 2]) & (rec[:, 5] > rec[:, 3]) & (rec[:, 0] >= 0)
+    if times is not None:
+        good &= rec[:, 0] < len(times)
+
+    def along(count, origin, size, n, pad):
+        g = np.arange(count)[None]
+        at = origin[:, None] + ((2 * g + 1) * p - 2 * pad[:, None]) * size[:, None] / (2 * n[:, None])
+        return at, (g * p < pad[:, None] + n[:, None]) & ((g + 1) * p > pad[:, None])
+
+    x, vx = along(gw, rec[:, 2], rec[:, 4] - rec[:, 2], fit[:, 0], fit[:, 2])
+    y, vy = along(gh, rec[:, 3], rec[:, 5] - rec[:, 3], fit[:, 1], fit[:, 3])
+    pos = np.zeros((len(rec), gh, gw, 3))
+    if times is not None:
+        pos[..., 0] = np.where(good, times[np.clip(rec[:, 0], 0, len(times) - 1)], 0)[:, None, None]
+    pos[..., 1], pos[..., 2] = y[:, :, None], x[:, None, :]
+    pos[~good] = 0
+    vis = (vy[:, :, None] & vx[:, None, :] & good[:, None, None]).astype(np.uint8)
+    return pos.reshape(len(rec), gh * gw, 3), vis.reshape(len(rec), gh * gw)
+
+
+@pytest.mark.parametrize("slot,patch", [((224, 224), 16), ((96, 33), 3), ((2048, 16), 8), ((64, 2048), 64), ((24, 40), 8),
+                                        ((8, 1), 1), ((2048, 8), 1)])
+@pytest.mark.parametrize("keep", [False, True])
+@pytest.mark.parametrize("n", [37, 301, 1000])
+def test_positions_of_batches(slot, patch, keep, n):
+    """Batches that give a warp to an item (from two items per SM on, unless an item's table is long), with times, records that
+    are no items between good ones, a count that ends inside a CTA, outputs at odd places, and rectangles up to 2^30 a side."""
+    rng = np.random.default_rng(n + patch)
+    rec = np.zeros((n, 8), np.int32)
+    rec[:, 0] = rng.integers(0, 5, n)
+    rec[:, 2:4] = rng.integers(0, 9000, (n, 2))
+    rec[:, 4:6] = rec[:, 2:4] + np.exp(rng.uniform(0, math.log(16384), (n, 2))).astype(np.int32)
+    far = rng.choice(n, n // 4, replace=False)
+    rec[far, 4:6] = rec[far, 2:4] + np.exp(rng.uniform(math.log(1 << 17), math.log(1 << 30), (len(far), 2))).astype(np.int32)
+    for k, at in enumerate(rng.choice(n, 12, replace=False)):
+        if k % 3 == 0:
+            rec[at, 4] = rec[at, 2] - k  # an empty rectangle
+        else:
+            rec[at, 0] = (-1, 5)[k % 2]  # no frame of that number
+    items, packed = torch.from_numpy(rec).cuda(), n - 3
+    patches = (slot[0] // patch) * (slot[1] // patch)
+    times = (rng.random(5) * 1e5).astype(np.float32)
+    want, wvis = _places(rec, slot, patch, keep, times)
+    for off in (0, 1):
+        pos = torch.full((n * patches * 3 + 4,), -5.0, device="cuda")[off:off + n * patches * 3]
+        vis = torch.full((n * patches + 4,), 9, dtype=torch.uint8, device="cuda")[off:off + n * patches]
+        octo.patch_positions(items, slot, patch, keep_aspect=keep, times=torch.from_numpy(times).cuda(), n_items=_ints([packed]),
+                             positions=pos, visible=vis)
+        assert (pos[packed * patches * 3:] == -5).all() and (vis[packed * patches:] == 9).all()
+        assert np.array_equal(vis[:packed * patches].cpu().numpy(), wvis[:packed].reshape(-1))
+        got = pos[:packed * patches * 3].cpu().numpy().astype(np.float64)
+        ref = want[:packed].reshape(-1)
+        assert (np.abs(got - ref) <= 2.0**-24 * np.abs(ref) * (1 + 1e-6) + 1e-9).all()
