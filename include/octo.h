@@ -512,9 +512,10 @@ typedef struct {
  * of the first 2 * pairs elements, (i, i + pairs) or with `interleaved` (2 i, 2 i + 1), is turned by the angle
  * position[axis[i]] * freq[i]: (y0 cos - y1 sin, y1 cos + y0 sin); elements from 2 * pairs on and pairs of an axis
  * that is not there stay y, whatever lies beside them.
- * The angle is reduced in 46 bits or more (a position of 2^24 and a frequency of 1 still have a phase that is good
- * to binary32); everything else is binary32, rounded once to the type of the tensors.  For the 16-bit types sine
- * and cosine are off by up to 2^-21.
+ * The angle's whole turns are taken off in 46 bits or more (a position of 2^24 and a frequency of 1 still have a phase
+ * that is good to binary32); everything else is binary32, rounded once to the type of the tensors.  For the 16-bit types
+ * sine and cosine are off by up to 1.4e-6 (2^-19.4): 2^-21.2 from the functions, the rest from the angle, which is
+ * rounded to binary32.
  */
 typedef struct {
     int32_t device, dtype;            /* OCTO_F16, OCTO_BF16 or OCTO_F32                                   */

@@ -195,3 +195,32 @@ def test_attention_looks_through_a_billion_hidden_keys():
     assert ((out[q_rows:].double() - v[:1].double()).abs() <= (2 * _u(BF16) + 2.0**-15) * v[:1].double().abs()).all()
     del mask
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("turns", [0.5, 16.0, 2.0**12, 2.0**22, 2.0**27])
+@pytest.mark.parametrize("whole", [False, True])
+def test_sine_and_cosine_of_the_rotation(dtype, turns, whole):
+    """Cosine and sine, read from heads of (1, 0), against the stated bounds.
+
+    binary32: two units of sincospif (2^-22) and the angle, taken off its whole turns with 2^-46 of them (2 pi 2^-46 turns;
+    beyond 2^22 turns in binary64, 2^-51).  16 bits: __sinf and __cosf are off by up to 2^-21.19 (4.2e-7); the turns' rest is
+    rounded to binary32 once (2^-25 turns, 1.9e-7; near 2^22 turns 2^-24, 3.8e-7) and multiplied by 2 pi (half a step below 4,
+    1.2e-7, and the constant's 2^-25.1 of up to pi, 0.9e-7), and the reduction is off by up to 3.8e-7 there: 1.4e-6 in all.  The
+    output's rounding hides that except near the zeros, which is where a part of these angles lies."""
+    rows, pairs = 60000, 128
+    g = _gen(int(turns) + 7)
+    q = torch.zeros((rows, 1, 2 * pairs), device="cuda", dtype=dtype)
+    q[..., :pairs] = 1
+    pos = torch.randint(-(1 << 24), 1 << 24, (rows, 1), generator=g, device="cuda").int()
+    freqs = torch.rand(pairs, generator=g, device="cuda") * (turns * 2 * math.pi / 2**24)
+    axes = torch.zeros(pairs, dtype=torch.int32, device="cuda")
+    out, _ = octo.norm_rotate(q, None, pos if whole else pos.float(), freqs, axes)
+    angle = pos.double() * freqs.double()  # (exact)
+    want = torch.cat([angle.cos(), angle.sin()], -1)
+    off = 2 * math.pi * min(turns * 2.0**-46, 2.0**-24) + turns * 2 * math.pi * 2.0**-51
+    tol = 2.0**-22 + off if dtype == F32 else 1.4e-6 + turns * 2 * math.pi * 2.0**-51
+    tol = tol + _u(dtype) * want.abs() + (2.0**-25 if dtype == F16 else 0.0)
+    err = (out[:, 0].double() - want).abs()
+    assert (err <= tol).all(), float((err - tol).max())
+    assert int((want.abs() < 2.0**-12).sum()) > 1000
