@@ -229,7 +229,7 @@ __device__ __forceinline__ Run<T, N> run_down(const float* f) {
 }
 
 // Sine and cosine of position * freq, from the whole turns' remainder.  In binary64 (the product of two binary32
-// numbers is exact) for positions of any size ...
+// numbers is exact, of an int32 and a binary32 number off by 2^-53) for positions of any size ...
 __device__ __noinline__ void turn_far(double position, float freq, float& c, float& s) {
     const double turns = position * (double)freq * 0.15915494309189533577;
     const double half_turns = 2.0 * (turns - rint(turns));  // in [-1, 1]
@@ -336,7 +336,7 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lanes, int heads_per_group)
                     const int64_t at = row * a.num_axes + axis;
                     if (a.positions_are_int) {
                         const int pos = static_cast<const int*>(a.positions)[at];
-                        if (abs(pos) <= 1 << 24) turn_of<sizeof(T) == 2>((float)pos, a.freqs[p + j], c, s);
+                        if (pos >= -(1 << 24) && pos <= 1 << 24) turn_of<sizeof(T) == 2>((float)pos, a.freqs[p + j], c, s);
                         else turn_far((double)pos, a.freqs[p + j], c, s);
                     } else {
                         turn_of<sizeof(T) == 2>(static_cast<const float*>(a.positions)[at], a.freqs[p + j], c, s);

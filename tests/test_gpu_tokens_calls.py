@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2502_01277_b200 as octo
-from test_gpu_tokens import BF16, F16, F32, _attend_ref, _gen, _ints, _qkv, _u
+from test_gpu_tokens import BF16, F16, F32, _attend_ref, _gen, _ints, _qkv, _rotate_check, _rotate_ref, _u
 
 pytestmark = pytest.mark.gpu
 
@@ -224,3 +224,15 @@ def test_sine_and_cosine_of_the_rotation(dtype, turns, whole):
     err = (out[:, 0].double() - want).abs()
     assert (err <= tol).all(), float((err - tol).max())
     assert int((want.abs() < 2.0**-12).sum()) > 1000
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rotation_by_the_ends_of_int32(dtype):
+    """(The smallest int32 has no absolute value.)"""
+    ends = [-(1 << 31), -(1 << 31) + 1, (1 << 31) - 1, -(1 << 24) - 1, -(1 << 24), (1 << 24) + 1, 0]
+    pos, g = _ints([[p] for p in ends]), _gen(31)
+    q = torch.randn((len(ends), 2, 64), generator=g, device="cuda").to(dtype)
+    freqs, axes = torch.rand(32, generator=g, device="cuda") * 2.0**-20, torch.zeros(32, dtype=torch.int32, device="cuda")
+    out, _ = octo.norm_rotate(q, None, pos, freqs, axes)
+    want, size = _rotate_ref(q, None, pos, freqs, axes, 1e-6, False)
+    _rotate_check(out, want, size, dtype)
