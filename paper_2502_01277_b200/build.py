@@ -4,9 +4,11 @@ the result is a plain C-ABI shared object next to the sources.
     python -m paper_2502_01277_b200.build [--force] [--ptxas] [--checked]
 
 --checked builds liboctostage_checked.so with -DOCTO_BOUNDS_CHECK: the same library with every
-computed shared- and global-memory index of the kernels range-checked; a miss sets
-OCTO_STATUS_BOUNDS in the status word and skips the access (no trap).  It stands in for a
-memory checker where none can be run; tests load it with load_library(path)."""
+computed shared- and global-memory index of the stage's and the attention kernels range-checked; a
+miss sets OCTO_STATUS_BOUNDS in the status word and skips the access (no trap).  (Positions and
+rotation have no status word: what they index by device data, an item's frame, a pair's axis and the
+count of items, is checked in every build, and the rest follows from checked arguments.)  It stands
+in for a memory checker where none can be run; tests load it with load_library(path)."""
 from __future__ import annotations
 
 import os
