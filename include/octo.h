@@ -556,7 +556,9 @@ OCTO_API int octo_rotate_plan(const octo_rotate_t* args, int32_t* run, int32_t* 
  * over the key rows j of r's segment with d_key_mask[j] != 0 (no mask: all of them); 0 where there is none.
  * Hidden keys and values are never looked at: they may hold NaN or infinities.  Rows of no segment are left
  * as they were.  Scores, the softmax and the sums are binary32; the weights are rounded to the tensors' type
- * before they meet the values, as the tensor cores take them; one rounding at the end.
+ * before they meet the values, as the tensor cores take them; one rounding at the end.  So a visible infinity among the
+ * values makes NaN where its weight rounds to zero (in fp16 below 2^-25 of the row's largest weight).  A row whose every
+ * score is minus infinity counts as one without visible keys.
  */
 typedef struct {
     int32_t device, dtype;            /* OCTO_F16 or OCTO_BF16                                             */
