@@ -404,10 +404,11 @@ static int make_plan(const octo_attend_t* c, int sms, AttendPlan* p) {
     const int64_t max_k = bound_of(c->max_k, c->d_k_offsets, c->k_rows, c->k_total);
     // Up to 16 rows a segment the step kernel reads every key once and is always ahead.  More rows take several of its
     // CTAs, which read the keys again, but a CTA is through in 3 us where a tile takes 7 to 9: it stays ahead while the
-    // whole call is small.  Work in key rows read, with what a CTA costs beside them (256); us tile / step:
-    // 4 segments of 64 rows, 8 key heads of 128, 512 keys 14.1 / 10.0, 2048 keys 18.4 / 26.4; 64 segments of 32 rows, 128
-    // keys 22.9 / 21.5, 512 keys 43 / 54; 64 of 64 rows, 8 key heads of 64, 128 keys 20.9 / 20.7; 8 of 128 rows, 2 key heads,
-    // 512 keys 12.9 / 8.3.
+    // whole call is small.  Work in key rows read, with what a CTA costs beside them (256); us on the GPU tile / step:
+    // 4 segments of 64 rows, 8 key heads of 128, 512 keys 13.9 / 9.5, 2048 keys 18.0 / 25.3; 64 segments of 32 rows, 128
+    // keys 22.8 / 19.4, 512 keys 42 / 53; 64 of 64 rows, 8 key heads of 64, 128 keys 20.6 / 19.8; 8 of 128 rows, 2 key heads,
+    // 512 keys 12.8 / 7.4.  Where it goes wrong: many segments of a dozen keys (216 of 28 rows and 18 keys, 16 heads of 64,
+    // 82 / 44), which count as large.
     const double step_ctas = (double)c->segments * c->kv_heads * (double)((max_q * group + kStepRows - 1) / kStepRows);
     const double work = step_ctas * (double)(max_k + 256) * (c->head_dim > 64 ? 2 : 1);
     p->tile = max_q * group > kStepRows && work > (step_ctas >= 4.0 * sms ? 800e3 : 300e3);
@@ -420,8 +421,9 @@ static int make_plan(const octo_attend_t* c, int sms, AttendPlan* p) {
     const int64_t busy = units < rows_make * c->kv_heads ? units : rows_make * c->kv_heads;
     // Work is split over the keys, into splits of one size.  Few rows: up to kStepFill CTAs per SM, 512 keys at least.  Tiles:
     // up to one per SM at 512 keys at least, and beyond that up to four per SM at 2048 keys at least, since tiles of
-    // uneven length on one CTA per SM end at different times (14 segments of 196 rows and one head, 32 000 keys: 138 us
-    // with one split size per SM, 88 so).
+    // uneven length on one CTA per SM end at different times.  us with up to one / up to four tiles per SM: 14 segments of 196
+    // rows and 8000 to 32 000 keys, heads of 64, four heads 246 / 211, one head whose longest segment is not known 343 / 175
+    // (where it is known 60 / 81: shorter splits than it needs); 5 segments of 300 rows, four heads of 128 190 / 147.
     auto at_most = [&](int64_t want, int64_t keys) {
         const int64_t a = want / busy, b = max_k / keys;
         return a < b ? a : b;

@@ -35,8 +35,10 @@ constexpr int kListInts = 256;
 constexpr float kMostInTurn = 1024.0f, kGrown = 4.0f;
 
 // Both halves begin an item together and stay in step, so that their exponentials share the special-function unit at one
-// time and leave it alone at another.  Half a turn of delay for the second half, once an item, sets them apart
-// (crops of 32 frames, heads of 128: 1680 -> 1590 us; 400, 1000 and 1400 clocks gave less).
+// time and leave it alone at another.  Half a turn of delay for the second half, once an item, sets them apart.
+// us without / with: crops of 32 frames, heads of 128, 1600 keys 1699 / 1589 at 1965 MHz (ten calls), 1927 / 1827 at
+// 1730 / 1660 MHz (1.5 s of calls, power cap); of 64 frames, 49 rows, heads of 64, 900 visible keys 552 / 542; ragged
+// items of a few turns, heads of 80 23.5 / 22.6 (400, 1000 and 1400 clocks gave less on the first).
 constexpr int kStagger = 700;
 
 template <int DB>
@@ -145,7 +147,7 @@ template <typename T>
 __device__ __forceinline__ void weigh(const uint32_t* s, unsigned long long scale, unsigned long long minus, uint32_t* p,
                                       unsigned long long& sum) {
     // (All exponents, then all exponentials, then sums and weights: left to itself the compiler went through pairs one
-    // after the other and waited for each; 1760 -> 1702 us.)
+    // after the other and waited for each: crops of 32 frames, heads of 128 1637 -> 1589 us at 1965 MHz; heads of 64 the same.)
     float e[32];
 #pragma unroll
     for (int i = 0; i < 16; ++i)

@@ -15,8 +15,8 @@ namespace octo {
 // Positions.  The threads of an item first make one coordinate per patch column and patch row (a division in
 // binary64 each, of which a patch of its own would need two), then write the item's block of (time, y, x) triples
 // with neighbouring threads on neighbouring words.  A batch of many items gives a warp to each, which lets all
-// of a server's batch be under way at once; a few items get a CTA each (7356 items of 196 patches, a call: 17.2 us with a CTA
-// per item, 11.8 with a warp; 9.4 with four words at a time, divisions in 32 bits).
+// of a server's batch be under way at once; a few items get a CTA each (7356 items of 196 patches: 13.1 us with a CTA
+// per item, 8.5 with a warp; 22 items 2.4).  What grows with the items is instructions: each word picks its source.
 // ---------------------------------------------------------------------------------------
 constexpr int kPosThreads = 128;
 constexpr int kPosMaxSide = 2048;  // patches along a side of a slot
@@ -468,9 +468,10 @@ static cudaError_t launch_rotate(const RotArgs& a, bool interleaved, int sm_coun
     }
     const int64_t blocks = (warps + kRotThreads / 32 - 1) / (kRotThreads / 32);
     const dim3 grid((unsigned)blocks, (unsigned)ceil_div(total, per));
-    // Heads in flight.  One head: one.  Runs of less than eight elements, or few heads: two, and more CTAs (us two / four:
-    // 137 000 tokens, 16 + 16 heads of 72 314 / 363; 196 000 tokens, 5 + 5 heads of 64 124 / 138).  Else what 16 registers of
-    // a lane hold (four of 16 bits, two of binary32; 274 000 tokens, 16 + 16 heads of 64 399, two 440).
+    // Heads in flight.  One head: one.  Few heads: two, and more CTAs (us two / four: 196 000 tokens, 5 + 5 heads of 64 129 / 135).
+    // Else what 16 registers of a lane hold (four of 16 bits, two of binary32; two / four: 274 000 tokens, 16 + 16 heads of 64
+    // 458 / 404).  Runs of less than eight elements: two (four took 303 instead of 324 for 137 000 tokens of 16 + 16 heads of 72;
+    // fewer heads were not compared).
     const int most = std::min(per, std::max(a.t[0].heads, a.t[1].heads));
     auto start = [&](auto batch) {
         constexpr int BATCH = decltype(batch)::value;
@@ -507,8 +508,8 @@ template <typename T>
 static cudaError_t rotate_typed(const octo_rotate_t& c, const RotArgs& a, int sm_count, cudaStream_t stream, RotateForm* form) {
     if (runs_of(c, a, 8, (int)sizeof(T))) return launch_rotate<T, 8, 1>(a, c.interleaved != 0, sm_count, stream, form);
     if (runs_of(c, a, 4, (int)sizeof(T))) return launch_rotate<T, 4, 1>(a, c.interleaved != 0, sm_count, stream, form);
-    // Shorter runs: two units per lane where a warp then takes two tokens rather than one (one fp32 head of 72 with 18
-    // turning pairs in q and k, 835 000 tokens: 1070 us with one unit, 620 with two).
+    // Shorter runs: two units per lane where a warp then takes two tokens or more rather than one (one fp32 head of 72 with
+    // 18 turning pairs in q and k, 835 000 tokens: 600 us with one unit, 269 with two).
     const int half = c.head_dim / 2;
     const bool ilv = c.interleaved != 0;
     if (runs_of(c, a, 2, (int)sizeof(T)))
