@@ -500,7 +500,8 @@ OCTO_API int octo_stage_patch_positions(octo_stage_t* st, int32_t branch, int32_
                                         void* cuda_stream);
 
 /* One tensor [rows, heads, head_dim] of a token call; the elements of a head lie side by side.  Rows or heads of an
- * input may lie on one another (a stride of 0), those of an output may not: such strides are refused. */
+ * input may lie on one another (a stride of 0), those of an output may not: strides less than head_dim apart from 0 or
+ * from one another are refused. */
 typedef struct {
     void* d_data;
     int64_t row_stride, head_stride; /* elements */

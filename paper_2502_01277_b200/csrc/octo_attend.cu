@@ -513,7 +513,7 @@ extern "C" int octo_cross_attention(const octo_attend_t* c, void* d_workspace, i
     for (const octo_heads_t* t : {&c->q, &c->k, &c->v, &c->out})
         for (int64_t s : {t->row_stride, t->head_stride})
             if (s < 0 || s >= (int64_t)1 << 30) return OCTO_E_INVALID_ARG;
-    if (rows_coincide(c->out, c->q_total, c->heads)) return OCTO_E_INVALID_ARG;
+    if (rows_coincide(c->out, c->q_total, c->heads, c->head_dim)) return OCTO_E_INVALID_ARG;
     if (!aligned_to(c->d_q_offsets, 4) || !aligned_to(c->d_k_offsets, 4) || !aligned_to(c->d_status, 4) ||
         !aligned_to(d_workspace, 16))
         return OCTO_E_ALIGNMENT;

@@ -561,7 +561,7 @@ static int rotate_call(const octo_rotate_t* c, void* cuda_stream, RotateForm* fo
     if (c->pairs > 0 && (!c->d_positions || !c->d_freqs || !c->d_axes)) return OCTO_E_INVALID_ARG;
     if (c->heads > 0 && (!c->q.d_data || !c->q_out.d_data)) return OCTO_E_INVALID_ARG;
     if (c->kv_heads > 0 && (!c->k.d_data || !c->k_out.d_data)) return OCTO_E_INVALID_ARG;
-    if (rows_coincide(c->q_out, c->rows, c->heads) || rows_coincide(c->k_out, c->rows, c->kv_heads)) return OCTO_E_INVALID_ARG;
+    if (rows_coincide(c->q_out, c->rows, c->heads, c->head_dim) || rows_coincide(c->k_out, c->rows, c->kv_heads, c->head_dim)) return OCTO_E_INVALID_ARG;
     const uintptr_t esize = c->dtype == OCTO_F32 ? 4 : 2;
     for (const void* p : {(const void*)c->q.d_data, (const void*)c->k.d_data, (const void*)c->q_out.d_data,
                           (const void*)c->k_out.d_data, c->d_q_weight, c->d_k_weight})

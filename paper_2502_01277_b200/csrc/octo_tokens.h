@@ -24,9 +24,13 @@ struct DeviceScope {
 };
 
 inline bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-// An output whose rows or heads lie on one another (an expanded tensor): which of them stayed would be a matter of time.
-inline bool rows_coincide(const octo_heads_t& t, int64_t rows, int heads) {
-    return rows > 0 && heads > 0 && ((t.row_stride == 0 && rows > 1) || (t.head_stride == 0 && heads > 1));
+// An output whose rows or heads lie on one another (an expanded tensor, windows of one that overlap, row r + 1 of head h in
+// the place of row r of head h + 1): what stayed there would be a matter of time.
+inline bool rows_coincide(const octo_heads_t& t, int64_t rows, int heads, int dim) {
+    auto near = [&](int64_t stride) { return stride > -dim && stride < dim; };
+    if (rows < 1 || heads < 1) return false;
+    return (rows > 1 && near(t.row_stride)) || (heads > 1 && near(t.head_stride)) ||
+           (rows > 1 && heads > 1 && (near(t.row_stride - t.head_stride) || near(t.row_stride + t.head_stride)));
 }
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 

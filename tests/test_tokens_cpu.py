@@ -198,3 +198,22 @@ def test_plans_null_and_empty(lib):
     assert lib.octo_rotate_plan(ctypes.byref(_rotate(head_dim=63)), *refs) == B.OCTO_E_INVALID_ARG
     a.value = b.value = c.value = 7
     assert lib.octo_rotate_plan(ctypes.byref(_rotate(rows=0)), *refs) == B.OCTO_OK and a.value == b.value == c.value == 0
+
+
+@pytest.mark.parametrize("over", [{"out.row_stride": 56}, {"out.head_stride": 8}, {"out.row_stride": 64, "out.head_stride": 64},
+                                  {"out.row_stride": 256, "out.head_stride": 312}])
+def test_attention_refuses_an_output_whose_rows_or_heads_overlap(lib, over):
+    assert lib.octo_cross_attention(ctypes.byref(_attend(**over)), None, 0, None) == B.OCTO_E_INVALID_ARG
+
+
+@pytest.mark.parametrize("over", [{"q_out.row_stride": 63}, {"k_out.head_stride": -1}, {"q_out.row_stride": 64, "q_out.head_stride": 100},
+                                  {"k_out.row_stride": -64}])
+def test_rotation_refuses_an_output_whose_rows_or_heads_overlap(lib, over):
+    assert lib.octo_norm_rotate(ctypes.byref(_rotate(**over)), None) == B.OCTO_E_INVALID_ARG
+
+
+@pytest.mark.parametrize("row,head", [(256, 64), (64, 512), (65, 4096), (-256, 64), (128, -64 * 6)])
+def test_outputs_of_any_order_are_taken(lib, row, head):
+    """(Accepted: the call goes on to a device that is not there.)"""
+    a = _rotate(device=1 << 20, **{"q_out.row_stride": row, "q_out.head_stride": head})
+    assert lib.octo_norm_rotate(ctypes.byref(a), None) == B.OCTO_E_CUDA
