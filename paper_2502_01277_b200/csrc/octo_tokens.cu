@@ -328,7 +328,7 @@ rotate_kernel(const __grid_constant__ RotArgs a, int lanes, int heads_per_group)
 #pragma unroll
         for (int j = 0; j < VP; ++j) {
             float c = 1.0f, s = 0.0f;
-            still |= 1u << (u * VP + j);
+            if (own[u]) still |= 1u << (u * VP + j);
             if (turning) {
                 const int axis = a.axes[p + j];
                 if (axis >= 0 && axis < a.num_axes) {
