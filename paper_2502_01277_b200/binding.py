@@ -552,9 +552,9 @@ class Stage:
                                   or times.device != self.device):
             raise OctoError(OCTO_E_INVALID_ARG, "octo_stage_patch_positions (times is not a float32 vector, one per frame)")
         if positions is None:
-            positions = _empty(t, (max_items, patches, 3), t.float32, self.device, stream)
+            positions = _empty(t, (max(max_items, 0), patches, 3), t.float32, self.device, stream)
         if visible is None:
-            visible = _empty(t, (max_items, patches), t.uint8, self.device, stream)
+            visible = _empty(t, (max(max_items, 0), patches), t.uint8, self.device, stream)
         for b, dtype, count in ((positions, t.float32, 3 * max_items * patches), (visible, t.uint8, max_items * patches)):
             if b.dtype != dtype or b.numel() < count or not b.is_contiguous() or b.device != self.device:
                 raise OctoError(OCTO_E_INVALID_ARG, "octo_stage_patch_positions (an output has another shape)")

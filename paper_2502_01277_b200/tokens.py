@@ -185,6 +185,8 @@ def cross_attention(q, k, v, segments: int, *, q_offsets=None, k_offsets=None, q
     k_total, kv, _ = k.shape
     if kv == 0 or heads % kv:
         _refuse(where, "kv_heads does not divide heads")
+    if dim == 0:
+        _refuse(where, "a head has no elements")
     if out is None:
         out = B._empty(t, (q_total, heads, dim), dtype, dev, stream)
     elif out.shape != q.shape or out.dtype is not dtype:

@@ -236,3 +236,25 @@ def test_rotation_by_the_ends_of_int32(dtype):
     out, _ = octo.norm_rotate(q, None, pos, freqs, axes)
     want, size = _rotate_ref(q, None, pos, freqs, axes, 1e-6, False)
     _rotate_check(out, want, size, dtype)
+
+
+def test_refusals_are_the_frameworks_own():
+    """Sizes of none and negative counts are refused as every other argument is, not by what trips over them."""
+    import workloads
+    from gpu_harness import make_stage, upload_frames
+    b = workloads.make_batch("two_branch", batch=3)
+    st = make_stage(b.workload, b.n)
+    frames, head = upload_frames(b.frames), torch.from_numpy(b.head).cuda()
+    st.preprocess(frames, b.sizes)
+    st.postprocess(head)
+    st.crop(0, 8)
+    q, k, v = _qkv(0, 4, 8, 4, 2, 64, BF16)
+    for call in (lambda: st.patch_positions(0, -1, 16), lambda: st.patch_positions(-1, 8, 16),
+                 lambda: octo.cross_attention(q[..., :0], k[..., :0], v[..., :0], 1, k_rows=8),
+                 lambda: octo.cross_attention(q, k, v, 1, k_rows=8, out=q[:1].expand(4, -1, -1)),
+                 lambda: octo.norm_rotate(q, None, torch.zeros((4, 1), device="cuda"), torch.zeros(2, device="cuda"),
+                                          _ints([0, 0]), out=(q[:1].expand(4, -1, -1), None))):
+        with pytest.raises(octo.OctoError) as e:
+            call()
+        assert e.value.code == octo.binding.OCTO_E_INVALID_ARG
+    st.close()
